@@ -71,12 +71,22 @@ typedef enum { EMB_POOL_SUM = 0, EMB_POOL_MEAN = 1 } emb_pool;
  * served from cache.  Results are bit-identical with and without it; quantised
  * tables ignore it. */
 #define EMB_ROWS_STREAMING 0x100
-/* Storage type of table rows.  EMB_INT8 / EMB_INT4 / EMB_INT4_ROW64 are
- * row-quantised tables (see emb_quantize_rows); only the forward lookup reads
- * those.  EMB_INT4_ROW64 holds the same scale, bias and codes as EMB_INT4 with
+/* Storage type of table rows.  EMB_INT8 / EMB_INT4 / EMB_INT4_ROW64 / EMB_MXFP4
+ * are row-quantised tables (see emb_quantize_rows); only the forward lookups (and
+ * emb_rows_product) read those.  EMB_INT4_ROW64 holds the same scale, bias and codes as EMB_INT4 with
  * every row padded to a multiple of 64 bytes: a choice for callers that prefer
- * lookup speed to table size (rows then never straddle a 64-byte sector). */
-typedef enum { EMB_F32 = 0, EMB_BF16 = 1, EMB_INT8 = 2, EMB_INT4 = 3, EMB_INT4_ROW64 = 4 } emb_dtype;
+ * lookup speed to table size (rows then never straddle a 64-byte sector).
+ * EMB_MXFP4 rows hold microscaled 4-bit floats: blocks of 32 elements share a
+ * power of two, and the matrix units read the rows as they are stored
+ * (emb_rows_product). */
+typedef enum {
+    EMB_F32 = 0,
+    EMB_BF16 = 1,
+    EMB_INT8 = 2,
+    EMB_INT4 = 3,
+    EMB_INT4_ROW64 = 4,
+    EMB_MXFP4 = 6
+} emb_dtype;
 
 /* bits of the device status word */
 #define EMB_STATUS_BAD_INDEX 1u   /* a row index < 0 or >= num_rows of its table */
@@ -133,12 +143,13 @@ int emb_lengths_to_offsets(const int32_t *lengths_dev, int64_t n, int64_t *offse
  * EMB_POOL_MEAN divides by the bag length; an empty bag gives zeros.  bf16
  * rows are widened exactly and accumulated in fp32; rows of a quantised table
  * (EMB_INT8, EMB_INT4) contribute scale * code + bias, dequantised in fp32
- * while they are gathered; out is fp32 [T,B,D] and is fully overwritten.
+ * while they are gathered (EMB_MXFP4: scale * code, exactly); out is fp32 [T,B,D] and is fully overwritten.
  * A bag's rows are added in the order of its lookups, here and in every other
  * lookup below: its bits do not depend on the other bags of the batch.
  * rows_dev: i64[nnz]; offsets_dev: i64[T*B+1].
  * EMB_ERR_UNSUPPORTED if D*element_size is not a multiple of 16 or exceeds
- * 16384 bytes (quantised: D not a multiple of 16 or above 1024), or T > 65535.
+ * 16384 bytes (quantised: D not a multiple of 16, EMB_MXFP4: of 32, or above
+ * 1024), or T > 65535.
  * B == 0 or T == 0 does nothing. */
 int emb_bag_forward(const emb_table *tables_host, const emb_table *tables_dev, int32_t T,
                     int32_t D, int32_t dtype, const int64_t *rows_dev,
@@ -369,7 +380,15 @@ int emb_bag_forward_mixed(const emb_table *tables_host, const emb_table *tables_
  *   of byte k (INT4, INT4_ROW64); zero padding.  Element value = scale * code
  *   + bias.
  * D = 64: 48 bytes for INT4, 37.5 % of an fp16 row; 64 bytes for INT4_ROW64,
- * 50 %.  0 on invalid arguments. */
+ * 50 %.
+ * EMB_MXFP4: D/2 + D/32 rounded up to a multiple of 16 (D a multiple of 32): the
+ * codes, element 2k in the low and 2k+1 in the high nibble of byte k, then one
+ * scale byte per block of 32 consecutive elements; zero padding.  A code is a
+ * 4-bit float: bit 3 the sign, bits 0..2 the magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ * a scale byte s stands for 2^(s - 127), s = 255 for not a number.  Element value
+ * = scale * code, exact in fp32 and in bf16 (beyond their range: infinite).  This
+ * is the block format MXFP4 of the OCP Microscaling Formats specification 1.0.
+ * 0 on invalid arguments. */
 int64_t emb_row_bytes(int32_t D, int32_t dtype);
 
 /* Post-training quantisation of an fp32 table [num_rows, D] (src_dev) into
@@ -377,12 +396,60 @@ int64_t emb_row_bytes(int32_t D, int32_t dtype);
  * asymmetric min/max, all in fp32 with IEEE division and round-half-even:
  *   bias = min_d x_d, scale = (max_d x_d - bias) / (2^b - 1), or 1 if the row
  *   is constant, code_d = clamp(rint((x_d - bias) / scale), 0, 2^b - 1).
- * dtype: EMB_INT8, EMB_INT4 or EMB_INT4_ROW64 (the codes of EMB_INT4, wider
- * padding).  Both pointers 16-byte aligned; dst_dev may be mapped host memory
- * (the rows are then written over the link).
- * EMB_ERR_UNSUPPORTED if D is not a multiple of 16 or above 1024. */
+ * EMB_MXFP4, block by block, in the manner that specification suggests:
+ *   scale = 2^e, e = floor(log2(max_d |x_d|)) - 2 brought into [-127, 127],
+ *   code_d = x_d / scale rounded to the nearest 4-bit float, ties to the one whose
+ *   lowest bit is 0, magnitudes above 6 becoming 6; the sign of a zero is kept.
+ *   A block of zeros has scale byte 0; a block that holds an infinity or a NaN has
+ *   scale byte 255 and codes 0, so that all its elements read as NaN.
+ * dtype: EMB_INT8, EMB_INT4, EMB_INT4_ROW64 (the codes of EMB_INT4, wider
+ * padding) or EMB_MXFP4.  Both pointers 16-byte aligned; dst_dev may be mapped
+ * host memory (the rows are then written over the link).
+ * EMB_ERR_UNSUPPORTED if D is not a multiple of 16 or above 1024 (EMB_MXFP4: not a
+ * multiple of 32 or above 65536; the lookups read rows of up to 1024 elements of
+ * every quantised type), or num_rows is 2^31 or more. */
 int emb_quantize_rows(const float *src_dev, int64_t num_rows, int32_t D, int32_t dtype,
                       void *dst_dev, void *stream);
+
+/* emb_quantize_rows from rows of either trained type, which need not lie next to
+ * each other: element d of row r is src_dev[r * src_stride + d] (src_stride in
+ * elements, >= D; src_stride * element size a multiple of 16).  src_dtype:
+ * EMB_F32 or EMB_BF16 (widened exactly, so that the codes are those of the widened
+ * rows): a bf16 table after training, a batch of pooled rows, or one feature's
+ * columns of a concatenated vector (emb_bag_forward_mixed).  dst_dev must not
+ * overlap the source. */
+int emb_quantize_rows_from(const void *src_dev, int32_t src_dtype, int64_t src_stride,
+                           int64_t num_rows, int32_t D, int32_t dtype, void *dst_dev, void *stream);
+
+/* The rows read back: dst[r * dst_stride + d] = the value that element d of
+ * quantised row r stands for, computed in fp32 as the lookups compute it and
+ * rounded to nearest-even where dst_dtype is EMB_BF16 (an EMB_MXFP4 value is a
+ * bf16 value as it is).  dst_dtype: EMB_F32 or EMB_BF16; dst_stride in elements,
+ * >= D, a multiple of 16 bytes; elements between the rows are not written.
+ * Shapes, alignment and errors as for emb_quantize_rows_from. */
+int emb_dequantize_rows(const void *src_dev, int32_t dtype, int64_t num_rows, int32_t D,
+                        void *dst_dev, int32_t dst_dtype, int64_t dst_stride, void *stream);
+
+/* Product with the rows of an EMB_MXFP4 table (Sections 3.1, 4.1.2: scores of
+ * vectors against the rows of a table stored in 4 bits, or a dense layer of the
+ * ranking model over pooled rows):
+ *   out[m * out_stride + n] = sum_{d < D} x[m, d] * W[n, d],  m < M, n < N
+ * w_rows_dev: N rows of emb_row_bytes(D, EMB_MXFP4).  x_dtype: EMB_F32 or EMB_BF16,
+ * element d of row m at x_dev[m * x_stride + d] (x_stride in elements, >= D;
+ * x_stride * element size a multiple of 16), taken as they are; or EMB_MXFP4, M rows
+ * of emb_row_bytes(D, EMB_MXFP4) (x_stride is ignored), as emb_quantize_rows_from
+ * makes them.  Both sides' values enter the products exactly (parts of an fp32 x
+ * below the smallest bf16, 2^-133, excepted); products are summed in fp32 by the
+ * matrix units, in an order that depends on the sizes alone, so the result is
+ * deterministic.  out_dtype: EMB_F32, or EMB_BF16 (the sum rounded to
+ * nearest-even once); out_stride in elements, >= N; elements between the rows are
+ * not written.  A NaN or infinity of x or W reaches the sums it takes part in, as in
+ * fp32.  x_dev and w_rows_dev 16-byte aligned; out_dev aligned to its elements; it
+ * must not overlap them.  Any M and N from 0 up to 2^31 - 1.
+ * EMB_ERR_UNSUPPORTED if D is not a multiple of 32 or above 65536. */
+int emb_rows_product(const void *x_dev, int32_t x_dtype, int64_t x_stride, int64_t M,
+                     const void *w_rows_dev, int64_t N, int32_t D, void *out_dev,
+                     int32_t out_dtype, int64_t out_stride, void *stream);
 
 /* The lookup of a training step (Section 3.1: the tables are fine-tuned inside
  * the ranking model, so every lookup is followed by its backward):
@@ -487,6 +554,51 @@ int emb_cache_index_bytes(int64_t num_rows, size_t *bytes);
 int emb_cache_build(const void *table_dev, int64_t num_rows, int32_t D, int32_t dtype,
                     const int64_t *hot_rows_dev, int64_t num_hot, void *cache_rows_dev,
                     void *cache_index_dev, uint32_t *status_dev, void *stream);
+
+/* A cache of fewer bits than its table (Sections 3.3, 4.1.2): emb_cache_build
+ * whose rows are quantised as they are written.  The table is EMB_F32 or EMB_BF16
+ * (dtype); cache row k is row hot_rows[k] in the storage type cache_dtype (EMB_INT8,
+ * EMB_INT4, EMB_INT4_ROW64 or EMB_MXFP4), byte for byte as emb_quantize_rows_from
+ * makes it (the storage of a bad entry of hot_rows_dev is left as it was).
+ * cache_rows_dev: num_hot rows of emb_row_bytes(D, cache_dtype); the index and
+ * everything else as for emb_cache_build.  Read by the
+ * emb_bag_forward_cached_quantized calls only.  EMB_ERR_UNSUPPORTED if D does not
+ * suit the cache's type (see emb_bag_forward) or the table's. */
+int emb_cache_build_quantized(const void *table_dev, int64_t num_rows, int32_t D, int32_t dtype,
+                              int32_t cache_dtype, const int64_t *hot_rows_dev, int64_t num_hot,
+                              void *cache_rows_dev, void *cache_index_dev, uint32_t *status_dev,
+                              void *stream);
+
+/* emb_cache_rebuild for such a cache: rows that the older cache (same table, same
+ * cache_dtype) holds are copied as they are, in HBM; the others are read from the
+ * table and quantised.  Arguments as for emb_cache_rebuild. */
+int emb_cache_rebuild_quantized(const void *table_dev, int64_t num_rows, int32_t D, int32_t dtype,
+                                int32_t cache_dtype, const void *old_cache_rows_dev,
+                                const void *old_cache_index_dev, int64_t old_num_hot,
+                                const int64_t *hot_rows_dev, int64_t num_hot, void *cache_rows_dev,
+                                void *cache_index_dev, uint64_t *moved_dev, uint32_t *status_dev,
+                                void *stream);
+
+/* emb_bag_forward_cached / _cached_hashed over a table and a cache of it that
+ * emb_cache_build_quantized or emb_cache_rebuild_quantized made: a lookup of a cached row contributes the
+ * value that the quantised row stands for (as in emb_bag_forward over a table of
+ * cache_dtype), any other the table's row in full precision, added in the order of
+ * the bag's lookups.  Everything else as for those two calls. */
+int emb_bag_forward_cached_quantized(const void *table_dev, int64_t num_rows, int32_t D,
+                                     int32_t dtype, int32_t cache_dtype,
+                                     const void *cache_rows_dev, const void *cache_index_dev,
+                                     int64_t num_hot, const int64_t *rows_dev,
+                                     const int64_t *offsets_dev, int64_t B, int64_t nnz,
+                                     int32_t mode, float *out_dev, uint64_t *hit_miss_dev,
+                                     uint32_t *status_dev, void *stream);
+int emb_bag_forward_cached_quantized_hashed(const void *table_dev, int64_t num_rows, int32_t D,
+                                            int32_t dtype, int32_t cache_dtype,
+                                            const void *cache_rows_dev,
+                                            const void *cache_index_dev, int64_t num_hot,
+                                            uint64_t salt, const uint64_t *raw_dev,
+                                            const int64_t *offsets_dev, int64_t B, int64_t nnz,
+                                            int32_t mode, float *out_dev, uint64_t *hit_miss_dev,
+                                            uint32_t *status_dev, void *stream);
 
 /* emb_bag_forward for one table whose rows are read from the HBM cache when
  * present and from table_dev (zero-copy over PCIe when it is mapped host

@@ -19,8 +19,9 @@ import torch
 from . import build as _build
 
 POOL = {"sum": 0, "mean": 1}
-DTYPE = {"f32": 0, "bf16": 1, "int8": 2, "int4": 3, "int4r64": 4}
-QUANT_DTYPES = ("int8", "int4", "int4r64")   # row-quantised storage; "int4r64": INT4 rows padded to 64 bytes
+DTYPE = {"f32": 0, "bf16": 1, "int8": 2, "int4": 3, "int4r64": 4, "mxfp4": 6}
+# row-quantised storage; "int4r64": INT4 rows padded to 64 bytes; "mxfp4": 4-bit floats, a power of two per 32 elements
+QUANT_DTYPES = ("int8", "int4", "int4r64", "mxfp4")
 ROWS_STREAMING = 0x100   # hint bit for the forward lookups (EMB_ROWS_STREAMING)
 STATUS_BAD_INDEX = 1
 STATUS_BAD_OFFSETS = 2
@@ -48,6 +49,8 @@ EXPORTS = [
     "emb_status_string", "emb_tables_init", "emb_hash_ids", "emb_hash_ids_tables", "emb_lengths_to_offsets",
     "emb_bag_forward", "emb_bag_forward_hashed", "emb_table_shapes_init", "emb_bag_forward_mixed", "emb_bag_backward_workspace_bytes", "emb_bag_backward_rowwise_adagrad",
     "emb_bag_backward_sort", "emb_debug_sort_poll_limit", "emb_bag_backward_update", "emb_bag_forward_train", "emb_bag_forward_train_lengths", "emb_offsets_scratch_bytes", "emb_bag_forward_hashed_lengths", "emb_bag_forward_lengths", "emb_bag_backward_sort_prepared", "emb_row_bytes", "emb_quantize_rows",
+    "emb_quantize_rows_from", "emb_dequantize_rows", "emb_rows_product", "emb_cache_build_quantized", "emb_cache_rebuild_quantized",
+    "emb_bag_forward_cached_quantized", "emb_bag_forward_cached_quantized_hashed",
     "emb_side_stream_create", "emb_side_stream_destroy", "emb_side_stream_join", "emb_bag_forward_train_lengths_after", "emb_event_create", "emb_event_destroy", "emb_event_record",
     "emb_event_elapsed_ms",
     "emb_cache_index_bytes", "emb_cache_build", "emb_bag_forward_cached", "emb_bag_forward_cached_hashed", "emb_bag_forward_cached_hashed_lengths", "emb_host_device_pointer",
@@ -153,6 +156,21 @@ def lib() -> C.CDLL:
     L.emb_row_bytes.argtypes = [i32, i32]
     L.emb_quantize_rows.restype = C.c_int
     L.emb_quantize_rows.argtypes = [vp, i64, i32, i32, vp, vp]
+    L.emb_quantize_rows_from.restype = C.c_int
+    L.emb_quantize_rows_from.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp]
+    L.emb_dequantize_rows.restype = C.c_int
+    L.emb_dequantize_rows.argtypes = [vp, i32, i64, i32, vp, i32, i64, vp]
+    L.emb_rows_product.restype = C.c_int
+    L.emb_rows_product.argtypes = [vp, i32, i64, i64, vp, i64, i32, vp, i32, i64, vp]
+    L.emb_cache_build_quantized.restype = C.c_int
+    L.emb_cache_build_quantized.argtypes = [vp, i64, i32, i32, i32, vp, i64, vp, vp, vp, vp]
+    L.emb_cache_rebuild_quantized.restype = C.c_int
+    L.emb_cache_rebuild_quantized.argtypes = [vp, i64, i32, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+    L.emb_bag_forward_cached_quantized.restype = C.c_int
+    L.emb_bag_forward_cached_quantized.argtypes = [vp, i64, i32, i32, i32, vp, vp, i64, vp, vp, i64, i64, i32, vp, vp, vp, vp]
+    L.emb_bag_forward_cached_quantized_hashed.restype = C.c_int
+    L.emb_bag_forward_cached_quantized_hashed.argtypes = [vp, i64, i32, i32, i32, vp, vp, i64, u64, vp, vp, i64, i64, i32, vp,
+                                                          vp, vp, vp]
     L.emb_cache_index_bytes.restype = C.c_int
     L.emb_cache_index_bytes.argtypes = [i64, C.POINTER(sz)]
     L.emb_cache_build.restype = C.c_int
@@ -276,7 +294,7 @@ def _check(fn: str, rc: int) -> None:
 _U64 = (torch.int64, torch.uint64)
 _U32 = (torch.int32, torch.uint32)
 _TABLE_TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "int8": torch.uint8, "int4": torch.uint8,
-                "int4r64": torch.uint8}
+                "int4r64": torch.uint8, "mxfp4": torch.uint8}
 
 
 # ---------------------------------------------------------------------------
@@ -575,6 +593,63 @@ def emb_quantize_rows(src: torch.Tensor, dtype: str, dst) -> None:
                                                         _stream()))
 
 
+_PLAIN = {torch.float32: "f32", torch.bfloat16: "bf16"}
+
+
+def _rows_2d(t: torch.Tensor, name: str):
+    """Pointer, storage type, rows, columns and row stride of a device matrix of fp32 or bf16 whose rows are contiguous."""
+    if t.dtype not in _PLAIN or t.dim() != 2:
+        raise TypeError(f"{name} must be a matrix of float32 or bfloat16")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    R, D = int(t.shape[0]), int(t.shape[1])
+    if D > 1 and t.stride(1) != 1:
+        raise TypeError(f"{name} must have contiguous rows")
+    stride = int(t.stride(0)) if R > 1 else D   # (of a single row the stride says nothing)
+    return t.data_ptr(), DTYPE[_PLAIN[t.dtype]], R, D, stride
+
+
+def emb_quantize_rows_from(src: torch.Tensor, dtype: str, dst) -> None:
+    """fp32 or bf16 ``src`` [R, D], rows contiguous, any row stride of whole 16 bytes -> row-quantised ``dst`` as for
+    ``emb_quantize_rows``."""
+    ptr, sd, R, D, stride = _rows_2d(src, "src")
+    if isinstance(dst, int):
+        dptr = dst
+    else:
+        if dst.numel() != R * emb_row_bytes(D, dtype):
+            raise TypeError("dst must hold R * emb_row_bytes bytes")
+        dptr = _ptr(dst, torch.uint8, "dst")
+    _check("emb_quantize_rows_from", lib().emb_quantize_rows_from(ptr, sd, stride, R, D, DTYPE[dtype], dptr, _stream()))
+
+
+def emb_dequantize_rows(src: torch.Tensor, dtype: str, dst: torch.Tensor) -> None:
+    """Quantised rows ``src`` uint8 [R, emb_row_bytes(D, dtype)] -> the values they stand for, ``dst`` [R, D] fp32 or bf16,
+    rows contiguous, any row stride of whole 16 bytes."""
+    ptr, dd, R, D, stride = _rows_2d(dst, "dst")
+    if src.numel() != R * emb_row_bytes(D, dtype):
+        raise TypeError("src must hold R * emb_row_bytes bytes")
+    _check("emb_dequantize_rows", lib().emb_dequantize_rows(_ptr(src, torch.uint8, "src"), DTYPE[dtype], R, D, ptr, dd, stride,
+                                                            _stream()))
+
+
+def emb_rows_product(x: torch.Tensor, w: torch.Tensor, D: int, out: torch.Tensor) -> None:
+    """``out`` [M, N] = ``x`` times the rows of ``w`` transposed.  ``w``: MXFP4 rows of ``D`` elements, uint8
+    [N, emb_row_bytes(D, "mxfp4")].  ``x``: [M, D] fp32 or bf16 with contiguous rows, or MXFP4 rows like ``w``.  ``out``: fp32 or
+    bf16 with contiguous rows."""
+    row = emb_row_bytes(D, "mxfp4")
+    optr, od, M, N, ostride = _rows_2d(out, "out")
+    if w.dim() != 2 or tuple(w.shape) != (N, row):
+        raise TypeError("w must be [%d, %d]" % (N, row))
+    if x.dim() != 2 or x.shape[0] != M or x.shape[1] != (row if x.dtype is torch.uint8 else D):
+        raise TypeError("x must have %d rows of %d elements" % (M, D))
+    if x.dtype is torch.uint8:
+        xptr, xd, xstride = _ptr(x, torch.uint8, "x"), DTYPE["mxfp4"], 0
+    else:
+        xptr, xd, _, _, xstride = _rows_2d(x, "x")
+    _check("emb_rows_product", lib().emb_rows_product(xptr, xd, xstride, M, _ptr(w, torch.uint8, "w"), N, int(D), optr, od, ostride,
+                                                      _stream()))
+
+
 def emb_bag_backward_workspace_bytes(T: int, B: int, nnz: int, total_rows: int, D: int, dtype: str) -> int:
     return int(lib().emb_bag_backward_workspace_bytes(int(T), int(B), int(nnz), int(total_rows), int(D),
                                                       DTYPE[dtype]))
@@ -806,6 +881,61 @@ def emb_cache_build(table_ptr: int, num_rows: int, D: int, dtype: str, hot_rows:
         int(table_ptr), int(num_rows), int(D), DTYPE[dtype], _ptr(hot_rows, torch.int64, "hot_rows"),
         hot_rows.numel(), _ptr(cache_rows, _TABLE_TORCH[dtype], "cache_rows"),
         _ptr(cache_index, torch.uint8, "cache_index"), _ptr(status, torch.int32, "status"), _stream()))
+
+
+def emb_cache_build_quantized(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str, hot_rows: torch.Tensor,
+                              cache_rows: torch.Tensor, cache_index: torch.Tensor,
+                              status: Optional[torch.Tensor] = None) -> None:
+    """``emb_cache_build`` with rows of ``cache_dtype`` (a quantised type), made from the table's as they are written."""
+    if cache_rows.numel() < hot_rows.numel() * emb_row_bytes(D, cache_dtype):
+        raise TypeError("cache_rows too small")
+    _check("emb_cache_build_quantized", lib().emb_cache_build_quantized(
+        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], _ptr(hot_rows, torch.int64, "hot_rows"),
+        hot_rows.numel(), _ptr(cache_rows, torch.uint8, "cache_rows"), _ptr(cache_index, torch.uint8, "cache_index"),
+        _ptr(status, torch.int32, "status"), _stream()))
+
+
+def emb_cache_rebuild_quantized(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str,
+                                old_cache_rows: Optional[torch.Tensor], old_cache_index: torch.Tensor, old_num_hot: int,
+                                hot_rows: torch.Tensor, cache_rows: torch.Tensor, cache_index: torch.Tensor,
+                                moved: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    if cache_rows.numel() < hot_rows.numel() * emb_row_bytes(D, cache_dtype):
+        raise TypeError("cache_rows too small")
+    _check("emb_cache_rebuild_quantized", lib().emb_cache_rebuild_quantized(
+        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype],
+        _ptr(old_cache_rows, torch.uint8, "old_cache_rows"), _ptr(old_cache_index, torch.uint8, "old_cache_index"),
+        int(old_num_hot), _ptr(hot_rows, torch.int64, "hot_rows"), hot_rows.numel(),
+        _ptr(cache_rows, torch.uint8, "cache_rows"), _ptr(cache_index, torch.uint8, "cache_index"), _ptr(moved, _U64, "moved"),
+        _ptr(status, torch.int32, "status"), _stream()))
+
+
+def _forward_cached_quantized(fn: str, table_ptr, num_rows, D, dtype, cache_dtype, cache_rows, cache_index, num_hot, salt, ids,
+                              id_dtype, offsets, B, mode, out, hit_miss, status):
+    if offsets.numel() != B + 1 or out.numel() != B * D:
+        raise TypeError("shape mismatch")
+    _check(fn, getattr(lib(), fn)(
+        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], _ptr(cache_rows, torch.uint8, "cache_rows"),
+        _ptr(cache_index, torch.uint8, "cache_index"), int(num_hot), *salt, _ptr(ids, id_dtype, "ids"),
+        _ptr(offsets, torch.int64, "offsets"), int(B), ids.numel(), POOL[mode], _ptr(out, torch.float32, "out"),
+        _ptr(hit_miss, _U64, "hit_miss"), _ptr(status, torch.int32, "status"), _stream()))
+
+
+def emb_bag_forward_cached_quantized(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str,
+                                     cache_rows: torch.Tensor, cache_index: torch.Tensor, num_hot: int, rows: torch.Tensor,
+                                     offsets: torch.Tensor, B: int, mode: str, out: torch.Tensor,
+                                     hit_miss: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    _forward_cached_quantized("emb_bag_forward_cached_quantized", table_ptr, num_rows, D, dtype, cache_dtype, cache_rows,
+                              cache_index, num_hot, (), rows, torch.int64, offsets, B, mode, out, hit_miss, status)
+
+
+def emb_bag_forward_cached_quantized_hashed(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str,
+                                            cache_rows: torch.Tensor, cache_index: torch.Tensor, num_hot: int, salt: int,
+                                            raw: torch.Tensor, offsets: torch.Tensor, B: int, mode: str, out: torch.Tensor,
+                                            hit_miss: Optional[torch.Tensor] = None,
+                                            status: Optional[torch.Tensor] = None) -> None:
+    _forward_cached_quantized("emb_bag_forward_cached_quantized_hashed", table_ptr, num_rows, D, dtype, cache_dtype, cache_rows,
+                              cache_index, num_hot, (C.c_uint64(int(salt) % (1 << 64)),), raw, _U64, offsets, B, mode, out,
+                              hit_miss, status)
 
 
 def emb_bag_forward_cached(table_ptr: int, num_rows: int, D: int, dtype: str, cache_rows: torch.Tensor,

@@ -217,7 +217,7 @@ int launch_cached(bool bf16, hipStream_t s, const char *table, const char *cache
     return EMB_OK;
 }
 
-template <int LPR, int BITS, int UNROLL>
+template <int LPR, int FMT, int UNROLL>
 __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_quant_kernel(const char *__restrict__ table,
                                                                            const char *__restrict__ cache_rows,
                                                                            const CacheEntry *__restrict__ index,
@@ -240,11 +240,11 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_quant_kernel(const
     int64_t s, e;
     const int64_t b0 = (int64_t)blockIdx.x * GROUPS;
     cached_bag_bounds<LPR>(offsets, lengths, offsets_out, B, b0, B - b0, b < B, b, l, bounds, wave_sums, status, s, e);
-    gather_dequant_pool_range<LPR, BITS, UNROLL>(src, b < B, b, s, e, l, nnz, rows, D, mode, out, status);
+    gather_dequant_pool_range<LPR, FMT, UNROLL>(src, b < B, b, s, e, l, nnz, rows, D, mode, out, status);
     cache_add_hit_miss(src.hits, src.misses, hit_miss);
 }
 
-template <int BITS>
+template <int FMT>
 int dispatch_cached_quant(int lpr, hipStream_t s, const char *table, const char *cache_rows, const CacheEntry *index,
                           int64_t num_rows, int64_t num_hot, int64_t B, int64_t nnz, const int64_t *rows,
                           const int64_t *offsets, int32_t D, int64_t row_bytes, int32_t mode, float *out,
@@ -254,7 +254,7 @@ int dispatch_cached_quant(int lpr, hipStream_t s, const char *table, const char 
 #define EMB_CQ(L)                                                                                                   \
     do {                                                                                                            \
         constexpr int GROUPS = Q_BLOCK / L;                                                                         \
-        hipLaunchKernelGGL((bag_forward_cached_quant_kernel<L, BITS, 8>), dim3((unsigned)((B + GROUPS - 1) / GROUPS)), \
+        hipLaunchKernelGGL((bag_forward_cached_quant_kernel<L, FMT, 8>), dim3((unsigned)((B + GROUPS - 1) / GROUPS)), \
                            dim3(Q_BLOCK), 0, s, table, cache_rows, index, num_rows, num_hot, B, nnz, rows, offsets, D, \
                            row_bytes, mode, out, hit_miss, status, hashed, salt, magic, offsets_out, lengths);      \
         EMB_RETURN_IF_LAUNCH_FAILED();                                                                              \
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(CF_BLOCK) void bag_forward_cached_tables_kernel(
     cache_add_hit_miss(src.hits, src.misses, hit_miss);
 }
 
-template <int LPR, int BITS, int UNROLL>
+template <int LPR, int FMT, int UNROLL>
 __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_tables_quant_kernel(
     const emb_cached_table *__restrict__ tables, int64_t B, uint32_t blocks_per_table, int64_t nnz,
     const int64_t *__restrict__ ids, const int64_t *__restrict__ offsets, int32_t D, int64_t row_bytes, int32_t mode,
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_tables_quant_kerne
     const int64_t b0 = (int64_t)(blockIdx.x % blocks_per_table) * GROUPS;
     cached_bag_bounds<LPR>(offsets, lengths, offsets_out, (int64_t)T * B, (int64_t)t * B + b0, B - b0, b < B, bag, l, bounds, wave_sums,
                            status, s, e);
-    gather_dequant_pool_range<LPR, BITS, UNROLL>(src, b < B, bag, s, e, l, nnz, ids, D, mode, out, status);
+    gather_dequant_pool_range<LPR, FMT, UNROLL>(src, b < B, bag, s, e, l, nnz, ids, D, mode, out, status);
     cache_add_hit_miss(src.hits, src.misses, hit_miss);
 }
 
@@ -377,30 +377,30 @@ int launch_cached_tables(const CachedTablesArgs &a, bool bf16)
     return EMB_OK;
 }
 
-template <int LPR, int BITS>
+template <int LPR, int FMT>
 int launch_cached_tables_quant(const CachedTablesArgs &a)
 {
     constexpr int GROUPS = Q_BLOCK / LPR;
     const int64_t per_table = (a.B + GROUPS - 1) / GROUPS;
     if (per_table * a.T > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((bag_forward_cached_tables_quant_kernel<LPR, BITS, 8>), dim3((unsigned)(per_table * a.T)),
+    hipLaunchKernelGGL((bag_forward_cached_tables_quant_kernel<LPR, FMT, 8>), dim3((unsigned)(per_table * a.T)),
                        dim3(Q_BLOCK), 0, a.s, a.tables, a.B, (uint32_t)per_table, a.nnz, a.ids, a.offsets, a.D,
                        a.row_bytes, a.mode, a.out, a.hit_miss, a.status, a.hashed, a.T, a.offsets_out, a.lengths);
     EMB_RETURN_IF_LAUNCH_FAILED();
     return EMB_OK;
 }
 
-template <int BITS>
+template <int FMT>
 int dispatch_cached_tables_quant(int lpr, const CachedTablesArgs &a)
 {
     switch (lpr) {
-        case 1: return launch_cached_tables_quant<1, BITS>(a);
-        case 2: return launch_cached_tables_quant<2, BITS>(a);
-        case 4: return launch_cached_tables_quant<4, BITS>(a);
-        case 8: return launch_cached_tables_quant<8, BITS>(a);
-        case 16: return launch_cached_tables_quant<16, BITS>(a);
-        case 32: return launch_cached_tables_quant<32, BITS>(a);
-        default: return launch_cached_tables_quant<64, BITS>(a);
+        case 1: return launch_cached_tables_quant<1, FMT>(a);
+        case 2: return launch_cached_tables_quant<2, FMT>(a);
+        case 4: return launch_cached_tables_quant<4, FMT>(a);
+        case 8: return launch_cached_tables_quant<8, FMT>(a);
+        case 16: return launch_cached_tables_quant<16, FMT>(a);
+        case 32: return launch_cached_tables_quant<32, FMT>(a);
+        default: return launch_cached_tables_quant<64, FMT>(a);
     }
 }
 
@@ -454,15 +454,9 @@ int emb_check_cache_build(const void *table_dev, int64_t num_rows, int32_t D, in
     return EMB_OK;
 }
 
-static int cache_build_entry(const void *table_dev, int64_t num_rows, int32_t D, int32_t dtype,
-                             const void *old_rows_dev, const void *old_index_dev, int64_t old_num_hot,
-                             const int64_t *hot_rows_dev, int64_t num_hot, void *cache_rows_dev, void *cache_index_dev,
-                             uint64_t *moved_dev, uint32_t *status_dev, void *stream)
+int emb_cache_index_launch(int64_t num_rows, const int64_t *hot_rows_dev, int64_t num_hot, void *cache_index_dev,
+                           uint32_t *status_dev, hipStream_t s)
 {
-    const int rc = emb_check_cache_build(table_dev, num_rows, D, dtype, old_rows_dev, old_index_dev, old_num_hot,
-                                         hot_rows_dev, num_hot, cache_rows_dev, cache_index_dev);
-    if (rc != EMB_OK) return rc;
-    hipStream_t s = emb_stream(stream);
     const int64_t entries = (num_rows + 63) / 64;
     const int64_t cblocks = (entries + CB_BLOCK - 1) / CB_BLOCK;
     if (cblocks > 0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
@@ -474,6 +468,20 @@ static int cache_build_entry(const void *table_dev, int64_t num_rows, int32_t D,
     hipLaunchKernelGGL(cache_mark_kernel, dim3((unsigned)mblocks), dim3(CB_BLOCK), 0, s, hot_rows_dev, num_hot,
                        num_rows, reinterpret_cast<CacheEntry *>(cache_index_dev), status_dev);
     EMB_RETURN_IF_LAUNCH_FAILED();
+    return EMB_OK;
+}
+
+static int cache_build_entry(const void *table_dev, int64_t num_rows, int32_t D, int32_t dtype,
+                             const void *old_rows_dev, const void *old_index_dev, int64_t old_num_hot,
+                             const int64_t *hot_rows_dev, int64_t num_hot, void *cache_rows_dev, void *cache_index_dev,
+                             uint64_t *moved_dev, uint32_t *status_dev, void *stream)
+{
+    int rc = emb_check_cache_build(table_dev, num_rows, D, dtype, old_rows_dev, old_index_dev, old_num_hot,
+                                         hot_rows_dev, num_hot, cache_rows_dev, cache_index_dev);
+    if (rc != EMB_OK) return rc;
+    hipStream_t s = emb_stream(stream);
+    rc = emb_cache_index_launch(num_rows, hot_rows_dev, num_hot, cache_index_dev, status_dev, s);
+    if (rc != EMB_OK || num_hot == 0) return rc;
     const int chunks = (int)(emb_row_bytes(D, dtype) / 16);   // rows of every storage type are whole 16-byte chunks
     const int64_t want = (num_hot * chunks + COPY_BLOCK - 1) / COPY_BLOCK;
     const unsigned grid = (unsigned)(want > COPY_GRID ? COPY_GRID : want);
@@ -529,11 +537,15 @@ static int cached_entry(const void *table_dev, int64_t num_rows, int32_t D, int3
         const char *tp = reinterpret_cast<const char *>(table_dev), *cp = reinterpret_cast<const char *>(cache_rows_dev);
         const CacheEntry *ip = reinterpret_cast<const CacheEntry *>(cache_index_dev);
         unsigned long long *hm = reinterpret_cast<unsigned long long *>(hit_miss_dev);
-        if (emb_quant_bits(dtype) == 8)
-            return dispatch_cached_quant<8>(ql, s, tp, cp, ip, num_rows, num_hot, B, nnz, rows_dev, offsets_dev, D, rb,
-                                            mode, out_dev, hm, status_dev, hashed, salt, magic, offsets_out_dev, lengths_dev);
-        return dispatch_cached_quant<4>(ql, s, tp, cp, ip, num_rows, num_hot, B, nnz, rows_dev, offsets_dev, D, rb, mode,
-                                        out_dev, hm, status_dev, hashed, salt, magic, offsets_out_dev, lengths_dev);
+#define EMB_CQF(FMT)                                                                                                  \
+    return dispatch_cached_quant<FMT>(ql, s, tp, cp, ip, num_rows, num_hot, B, nnz, rows_dev, offsets_dev, D, rb, mode, \
+                                      out_dev, hm, status_dev, hashed, salt, magic, offsets_out_dev, lengths_dev)
+        switch (emb_quant_format(dtype)) {
+            case EMB_FMT_INT8: EMB_CQF(EMB_FMT_INT8);
+            case EMB_FMT_INT4: EMB_CQF(EMB_FMT_INT4);
+            default: EMB_CQF(EMB_FMT_MXFP4);
+        }
+#undef EMB_CQF
     }
     const int chunks = D * emb_elem_size(dtype) / 16;
     int lpr, cpl;
@@ -722,9 +734,14 @@ int emb_forward_cached_unchecked_tables(const emb_cached_table *td, int32_t T, i
     CachedTablesArgs a{td,      T,      B,         nnz,  ids_dev, offsets_dev, D, mode, emb_row_bytes(D, dtype),
                        out_dev, reinterpret_cast<unsigned long long *>(hit_miss_dev), status_dev, hashed, emb_stream(stream),
                        offsets_out_dev, lengths_dev};
-    if (emb_is_quant(dtype))
-        return emb_quant_bits(dtype) == 8 ? dispatch_cached_tables_quant<8>(emb_quant_lanes(D), a)
-                                          : dispatch_cached_tables_quant<4>(emb_quant_lanes(D), a);
+    if (emb_is_quant(dtype)) {
+        const int ql = emb_quant_lanes(D);
+        switch (emb_quant_format(dtype)) {
+            case EMB_FMT_INT8: return dispatch_cached_tables_quant<EMB_FMT_INT8>(ql, a);
+            case EMB_FMT_INT4: return dispatch_cached_tables_quant<EMB_FMT_INT4>(ql, a);
+            default: return dispatch_cached_tables_quant<EMB_FMT_MXFP4>(ql, a);
+        }
+    }
     int lpr, cpl;
     emb_row_split((int)(a.row_bytes / 16), lpr, cpl);
     const bool bf16 = dtype == EMB_BF16;

@@ -67,12 +67,31 @@ __device__ __forceinline__ void emb_bag_bounds(const int64_t *__restrict__ off, 
     }
 }
 
-// Quantised tables (quant.hip): shape check, and the pooled lookup emb_bag_forward hands over to.
+// Quantised tables (quant.hip): shape checks (of rows that a lookup reads, and of rows as such), and the pooled lookup
+// emb_bag_forward hands over to.
 int emb_check_quant_shape(int32_t D, int32_t dtype);
+int emb_check_quant_rows(int32_t D, int32_t dtype);
 int emb_forward_quant(const emb_table *tables_dev, int32_t T, int32_t D, int32_t dtype, const int64_t *rows_dev,
                       const int64_t *offsets_dev, int64_t B, int64_t nnz, int32_t mode, float *out_dev,
                       uint32_t *status_dev, hipStream_t s, bool hashed, int64_t *rows_out_dev,
                       int64_t *offsets_out_dev, const int32_t *lengths_dev);
+
+// Clears a cache index and marks the hot rows in it (cached.hip); the arguments have been checked.
+int emb_cache_index_launch(int64_t num_rows, const int64_t *hot_rows_dev, int64_t num_hot, void *cache_index_dev,
+                           uint32_t *status_dev, hipStream_t s);
+
+// Rows quantised (quant_rows.hip) after the arguments have been checked; src_pitch in bytes.  pick != NULL: row k of dst comes
+// from row hot[k] of src (nothing is written for an entry outside [0, num_rows)), or, where the older cache holds that
+// row already quantised (old_index != NULL), from there; moved (nullable): [0] += rows of the older cache, [1] += others.
+struct emb_row_pick {
+    const int64_t *hot;
+    int64_t num_rows;
+    const void *old_index, *old_rows;
+    int64_t old_num_hot;
+    uint64_t *moved;
+};
+int emb_quantize_launch(const void *src, int32_t src_dtype, int64_t src_pitch, int64_t R, int32_t D, int32_t dtype, void *dst,
+                        const emb_row_pick *pick, hipStream_t s);
 
 // emb_bag_forward / emb_bag_forward_hashed over descriptors that exist in device memory only and were
 // validated earlier (the latched copy of a version record; versioned.hip).
@@ -112,13 +131,17 @@ int emb_check_cache_build(const void *table_dev, int64_t num_rows, int32_t D, in
                           const void *old_index_dev, int64_t old_num_hot, const int64_t *hot_rows_dev, int64_t num_hot,
                           const void *cache_rows_dev, const void *cache_index_dev);
 
-// Row-quantised storage types and the bits of one of their codes (EMB_INT4_ROW64
+// Row-quantised storage types and how the kernels read their rows (EMB_INT4_ROW64
 // differs from EMB_INT4 in the row stride only).
+constexpr int EMB_FMT_INT8 = 8, EMB_FMT_INT4 = 4, EMB_FMT_MXFP4 = 40;
 static inline bool emb_is_quant(int32_t dtype)
 {
-    return dtype == EMB_INT8 || dtype == EMB_INT4 || dtype == EMB_INT4_ROW64;
+    return dtype == EMB_INT8 || dtype == EMB_INT4 || dtype == EMB_INT4_ROW64 || dtype == EMB_MXFP4;
 }
-static inline int emb_quant_bits(int32_t dtype) { return dtype == EMB_INT8 ? 8 : 4; }
+static inline int emb_quant_format(int32_t dtype)
+{
+    return dtype == EMB_INT8 ? EMB_FMT_INT8 : (dtype == EMB_MXFP4 ? EMB_FMT_MXFP4 : EMB_FMT_INT4);
+}
 
 // Row shape accepted by the gather kernels: whole 16-byte chunks, at most 1024 of them.
 // Quantised rows are read by the forward lookup only.

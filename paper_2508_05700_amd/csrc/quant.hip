@@ -1,99 +1,25 @@
 // Row-quantised tables (paper Section 4.1.2: the hosted tables are stored as
-// INT4 after post-training quantisation): the row-wise min/max quantiser and
-// the pooled lookup that dequantises while it gathers.
+// INT4 after post-training quantisation): the pooled lookup that dequantises
+// while it gathers.  (The quantisers are in quant_rows.hip.)
 //
 // Storage of one row of D elements, b = 8 or 4 bits per code:
 //   bytes 0..3 scale (fp32), bytes 4..7 bias (fp32), then the codes (INT8: one
 //   byte per element; INT4: element 2k in the low nibble of byte k, 2k+1 in the
 //   high nibble), zero-padded to a multiple of 16 bytes (EMB_INT4_ROW64: of 64
 //   bytes, otherwise the row of EMB_INT4).  Element value = scale * code + bias.
+// MXFP4: D/2 bytes of codes (nibbles in the same order, each a 4-bit float), then
+// one scale byte per 32 elements, zero-padded to a multiple of 16 bytes.  Codes
+// come first so that the 16 bytes of a block are aligned: the matrix units take
+// them as they are (product.hip).
 //
-// Both kernels give a lane 16 consecutive elements of a row, i.e. 8 (INT4) or
-// 16 (INT8) code bytes, so a row of D elements takes LPR = D/16 lanes rounded up
-// to a power of two; D must be a multiple of 16 and at most 1024.
+// The kernel gives a lane 16 consecutive elements of a row, i.e. 8 (INT4, MXFP4)
+// or 16 (INT8) code bytes, so a row of D elements takes LPR = D/16 lanes rounded up
+// to a power of two; D must be a multiple of 16 (MXFP4: 32) and at most 1024.
 #include "emb_internal.h"
 #include "gather_quant.h"
 #include "u64mod.h"
 
 namespace {
-
-// ---------------------------------------------------------------------------
-// quantiser
-// ---------------------------------------------------------------------------
-template <int LPR, int BITS>
-__global__ __launch_bounds__(Q_BLOCK) void quantize_rows_kernel(const float *__restrict__ src, int64_t R, int32_t D,
-                                                                int64_t row_bytes, char *__restrict__ dst)
-{
-    constexpr int GROUPS = Q_BLOCK / LPR;
-    constexpr float QMAX = BITS == 8 ? 255.0f : 15.0f;
-    const int l = threadIdx.x % LPR;
-    const int64_t r = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LPR;
-    const bool row_live = r < R;                 // whole lane groups share it
-    const bool live = row_live && l * Q_ELEMS < D;
-    float x[Q_ELEMS];
-    if (live) {
-        const float4 *p = reinterpret_cast<const float4 *>(src + r * D + l * Q_ELEMS);
-#pragma unroll
-        for (int i = 0; i < Q_ELEMS / 4; ++i) {
-            const float4 v = p[i];
-            x[4 * i + 0] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < Q_ELEMS; ++i) x[i] = 0.f;
-    }
-    // row minimum and maximum: exact, so the order of the comparisons does not matter
-    float lo = x[0], hi = x[0];
-#pragma unroll
-    for (int i = 1; i < Q_ELEMS; ++i) {
-        lo = x[i] < lo ? x[i] : lo;
-        hi = x[i] > hi ? x[i] : hi;
-    }
-    if (!live) {     // lanes past the row must not take part in min / max
-        lo = __builtin_inff();
-        hi = -__builtin_inff();
-    }
-#pragma unroll
-    for (int d = 1; d < LPR; d <<= 1) {
-        const float ol = __shfl_xor(lo, d, LPR), oh = __shfl_xor(hi, d, LPR);
-        lo = ol < lo ? ol : lo;
-        hi = oh > hi ? oh : hi;
-    }
-    if (!live) return;
-    // IEEE fp32 division and round-half-even, as the definition states
-    const float scale = hi == lo ? 1.0f : (hi - lo) / QMAX;
-    const float bias = lo;
-    uint32_t code[Q_ELEMS];
-#pragma unroll
-    for (int i = 0; i < Q_ELEMS; ++i) {
-        float q = rintf((x[i] - bias) / scale);
-        q = q < 0.0f ? 0.0f : q;
-        q = q > QMAX ? QMAX : q;
-        code[i] = (uint32_t)q;
-    }
-    char *row = dst + r * row_bytes;
-    if (BITS == 4) {
-        uint2 w = make_uint2(0u, 0u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w.x |= code[i] << (4 * i);
-            w.y |= code[8 + i] << (4 * i);
-        }
-        *reinterpret_cast<uint2 *>(row + 8 + l * 8) = w;
-    } else {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < Q_ELEMS; ++i) w[i / 4] |= code[i] << (8 * (i % 4));
-        *reinterpret_cast<uint2 *>(row + 8 + l * 16) = make_uint2(w[0], w[1]);
-        *reinterpret_cast<uint2 *>(row + 16 + l * 16) = make_uint2(w[2], w[3]);
-    }
-    if (l == 0) {
-        *reinterpret_cast<uint2 *>(row) = make_uint2(__float_as_uint(scale), __float_as_uint(bias));
-        // header and codes end on a multiple of 8 and so does the row: the padding is whole 8-byte words
-        for (int64_t at = 8 + (int64_t)D * BITS / 8; at < row_bytes; at += 8)
-            *reinterpret_cast<uint2 *>(row + at) = make_uint2(0u, 0u);
-    }
-}
 
 // ---------------------------------------------------------------------------
 // pooled lookup with dequantisation (the loop is in gather_quant.h)
@@ -130,7 +56,7 @@ struct HashedQuantTableSource {
 };
 
 // MAKE_OFFSETS: as in bag_forward_kernel (forward.hip).
-template <int LPR, int BITS, int UNROLL, bool HASHED, bool MAKE_OFFSETS>
+template <int LPR, int FMT, int UNROLL, bool HASHED, bool MAKE_OFFSETS>
 __global__ __launch_bounds__(Q_BLOCK) void bag_forward_quant_kernel(const emb_table *__restrict__ tables, int32_t T,
                                                                     int64_t B, uint32_t blocks_per_table, int64_t nnz,
                                                                     const int64_t *__restrict__ rows,
@@ -174,14 +100,14 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_quant_kernel(const emb_ta
     if (HASHED) {
         HashedQuantTableSource src{reinterpret_cast<const char *>(tb.weights), (uint64_t)tb.num_rows, tb.salt,
                                    tb.mod_magic, row_bytes, rows_out};
-        gather_dequant_pool_range<LPR, BITS, UNROLL>(src, live, bag, s, e, l, nnz, rows, D, mode, out, status);
+        gather_dequant_pool_range<LPR, FMT, UNROLL>(src, live, bag, s, e, l, nnz, rows, D, mode, out, status);
     } else {
         QuantTableSource src{reinterpret_cast<const char *>(tb.weights), (uint64_t)tb.num_rows, row_bytes, status};
-        gather_dequant_pool_range<LPR, BITS, UNROLL>(src, live, bag, s, e, l, nnz, rows, D, mode, out, status);
+        gather_dequant_pool_range<LPR, FMT, UNROLL>(src, live, bag, s, e, l, nnz, rows, D, mode, out, status);
     }
 }
 
-template <int LPR, int BITS>
+template <int LPR, int FMT>
 int launch_quant_forward(hipStream_t s, const emb_table *tables, int32_t T, int64_t B, int64_t nnz, const int64_t *rows,
                          const int64_t *offsets, int32_t D, int64_t row_bytes, int32_t mode, float *out,
                          uint32_t *status, bool hashed, int64_t *rows_out, int64_t *offsets_out, const int32_t *lengths)
@@ -192,7 +118,7 @@ int launch_quant_forward(hipStream_t s, const emb_table *tables, int32_t T, int6
     const int64_t blocks = emb_round_up_xcds(per_table * T);
     if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
 #define EMB_QK(HASHED, MAKE)                                                                                         \
-    hipLaunchKernelGGL((bag_forward_quant_kernel<LPR, BITS, UNROLL, HASHED, MAKE>), dim3((unsigned)blocks), dim3(Q_BLOCK), \
+    hipLaunchKernelGGL((bag_forward_quant_kernel<LPR, FMT, UNROLL, HASHED, MAKE>), dim3((unsigned)blocks), dim3(Q_BLOCK), \
                        0, s, tables, T, B, (uint32_t)per_table, nnz, rows, offsets, D, row_bytes, mode, out, status, \
                        rows_out, offsets_out, lengths)
     if (hashed) {
@@ -205,13 +131,13 @@ int launch_quant_forward(hipStream_t s, const emb_table *tables, int32_t T, int6
     return EMB_OK;
 }
 
-template <int BITS>
+template <int FMT>
 int dispatch_quant_forward(int lpr, hipStream_t s, const emb_table *tables, int32_t T, int64_t B, int64_t nnz,
                            const int64_t *rows, const int64_t *offsets, int32_t D, int64_t row_bytes, int32_t mode,
                            float *out, uint32_t *status, bool hashed, int64_t *rows_out, int64_t *offsets_out, const int32_t *lengths)
 {
 #define EMB_QF(L)                                                                                              \
-    return launch_quant_forward<L, BITS>(s, tables, T, B, nnz, rows, offsets, D, row_bytes, mode, out, status, \
+    return launch_quant_forward<L, FMT>(s, tables, T, B, nnz, rows, offsets, D, row_bytes, mode, out, status, \
                                          hashed, rows_out, offsets_out, lengths)
     switch (lpr) {
         case 1: EMB_QF(1);
@@ -225,36 +151,24 @@ int dispatch_quant_forward(int lpr, hipStream_t s, const emb_table *tables, int3
 #undef EMB_QF
 }
 
-template <int LPR, int BITS>
-void launch_quantize(hipStream_t s, const float *src, int64_t R, int32_t D, int64_t row_bytes, char *dst)
-{
-    constexpr int GROUPS = Q_BLOCK / LPR;
-    hipLaunchKernelGGL((quantize_rows_kernel<LPR, BITS>), dim3((unsigned)((R + GROUPS - 1) / GROUPS)), dim3(Q_BLOCK), 0,
-                       s, src, R, D, row_bytes, dst);
-}
-
-template <int BITS>
-void dispatch_quantize(int lpr, hipStream_t s, const float *src, int64_t R, int32_t D, int64_t row_bytes, char *dst)
-{
-    switch (lpr) {
-        case 1: return launch_quantize<1, BITS>(s, src, R, D, row_bytes, dst);
-        case 2: return launch_quantize<2, BITS>(s, src, R, D, row_bytes, dst);
-        case 4: return launch_quantize<4, BITS>(s, src, R, D, row_bytes, dst);
-        case 8: return launch_quantize<8, BITS>(s, src, R, D, row_bytes, dst);
-        case 16: return launch_quantize<16, BITS>(s, src, R, D, row_bytes, dst);
-        case 32: return launch_quantize<32, BITS>(s, src, R, D, row_bytes, dst);
-        default: return launch_quantize<64, BITS>(s, src, R, D, row_bytes, dst);
-    }
-}
-
 }  // namespace
 
-int emb_check_quant_shape(int32_t D, int32_t dtype)
+// Rows as such: INT8 / INT4 rows are made by a wavefront each, MXFP4 rows block by block.
+int emb_check_quant_rows(int32_t D, int32_t dtype)
 {
     if (!emb_is_quant(dtype)) return EMB_ERR_INVALID_ARG;
     if (D <= 0) return EMB_ERR_INVALID_ARG;
+    if (dtype == EMB_MXFP4) return D % 32 != 0 || D > 65536 ? EMB_ERR_UNSUPPORTED : EMB_OK;
     if (D % Q_ELEMS != 0 || D > Q_ELEMS * EMB_WAVE) return EMB_ERR_UNSUPPORTED;
     return EMB_OK;
+}
+
+// Rows that a lookup reads: at most a wavefront of lanes.
+int emb_check_quant_shape(int32_t D, int32_t dtype)
+{
+    const int rc = emb_check_quant_rows(D, dtype);
+    if (rc != EMB_OK) return rc;
+    return D > Q_ELEMS * EMB_WAVE ? EMB_ERR_UNSUPPORTED : EMB_OK;
 }
 
 extern "C" int64_t emb_row_bytes(int32_t D, int32_t dtype)
@@ -266,25 +180,9 @@ extern "C" int64_t emb_row_bytes(int32_t D, int32_t dtype)
         case EMB_INT8: return (8 + (int64_t)D + 15) / 16 * 16;
         case EMB_INT4: return D % 2 ? 0 : (8 + (int64_t)D / 2 + 15) / 16 * 16;
         case EMB_INT4_ROW64: return D % 2 ? 0 : (8 + (int64_t)D / 2 + 63) / 64 * 64;
+        case EMB_MXFP4: return D % 32 ? 0 : ((int64_t)D / 2 + D / 32 + 15) / 16 * 16;
         default: return 0;
     }
-}
-
-extern "C" int emb_quantize_rows(const float *src_dev, int64_t num_rows, int32_t D, int32_t dtype, void *dst_dev,
-                                 void *stream)
-{
-    if (num_rows < 0) return EMB_ERR_INVALID_ARG;
-    const int rc = emb_check_quant_shape(D, dtype);
-    if (rc != EMB_OK) return rc;
-    if (num_rows == 0) return EMB_OK;
-    if (!src_dev || !dst_dev || !emb_aligned(src_dev, 16) || !emb_aligned(dst_dev, 16)) return EMB_ERR_INVALID_ARG;
-    if (num_rows > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
-    const int64_t rb = emb_row_bytes(D, dtype);
-    hipStream_t s = emb_stream(stream);
-    if (emb_quant_bits(dtype) == 8) dispatch_quantize<8>(emb_quant_lanes(D), s, src_dev, num_rows, D, rb, static_cast<char *>(dst_dev));
-    else dispatch_quantize<4>(emb_quant_lanes(D), s, src_dev, num_rows, D, rb, static_cast<char *>(dst_dev));
-    EMB_RETURN_IF_LAUNCH_FAILED();
-    return EMB_OK;
 }
 
 // Called by emb_bag_forward (forward.hip) once the common arguments are checked.
@@ -298,9 +196,13 @@ int emb_forward_quant(const emb_table *tables_dev, int32_t T, int32_t D, int32_t
 {
     const int64_t rb = emb_row_bytes(D, dtype);
     const int lpr = emb_quant_lanes(D);
-    if (emb_quant_bits(dtype) == 8)
-        return dispatch_quant_forward<8>(lpr, s, tables_dev, T, B, nnz, rows_dev, offsets_dev, D, rb, mode, out_dev,
-                                         status_dev, hashed, rows_out_dev, offsets_out_dev, lengths_dev);
-    return dispatch_quant_forward<4>(lpr, s, tables_dev, T, B, nnz, rows_dev, offsets_dev, D, rb, mode, out_dev,
-                                     status_dev, hashed, rows_out_dev, offsets_out_dev, lengths_dev);
+#define EMB_QFF(FMT)                                                                                               \
+    return dispatch_quant_forward<FMT>(lpr, s, tables_dev, T, B, nnz, rows_dev, offsets_dev, D, rb, mode, out_dev,  \
+                                       status_dev, hashed, rows_out_dev, offsets_out_dev, lengths_dev)
+    switch (emb_quant_format(dtype)) {
+        case EMB_FMT_INT8: EMB_QFF(EMB_FMT_INT8);
+        case EMB_FMT_INT4: EMB_QFF(EMB_FMT_INT4);
+        default: EMB_QFF(EMB_FMT_MXFP4);
+    }
+#undef EMB_QFF
 }

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(SF_BLOCK) void bag_forward_staged_kernel(StagedSour
     cache_add_hit_miss(src.hits, src.misses, hit_miss);
 }
 
-template <int LPR, int BITS, int UNROLL>
+template <int LPR, int FMT, int UNROLL>
 __global__ __launch_bounds__(Q_BLOCK) void bag_forward_staged_quant_kernel(StagedSource src, int64_t B, int64_t nnz,
                                                                            const int64_t *__restrict__ loc,
                                                                            const int64_t *__restrict__ offsets,
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_staged_quant_kernel(Stage
     constexpr int GROUPS = Q_BLOCK / LPR;
     const int l = threadIdx.x % LPR;
     const int64_t b = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LPR;
-    gather_dequant_pool_bag<LPR, BITS, UNROLL>(src, b < B, b, l, nnz, loc, offsets, D, mode, out, status);
+    gather_dequant_pool_bag<LPR, FMT, UNROLL>(src, b < B, b, l, nnz, loc, offsets, D, mode, out, status);
     cache_add_hit_miss(src.hits, src.misses, hit_miss);
 }
 
@@ -215,28 +215,28 @@ int launch_staged(const StagedArgs &a, bool bf16)
     return EMB_OK;
 }
 
-template <int LPR, int BITS>
+template <int LPR, int FMT>
 int launch_staged_quant(const StagedArgs &a)
 {
     constexpr int GROUPS = Q_BLOCK / LPR;
-    hipLaunchKernelGGL((bag_forward_staged_quant_kernel<LPR, BITS, 8>), dim3((unsigned)((a.B + GROUPS - 1) / GROUPS)),
+    hipLaunchKernelGGL((bag_forward_staged_quant_kernel<LPR, FMT, 8>), dim3((unsigned)((a.B + GROUPS - 1) / GROUPS)),
                        dim3(Q_BLOCK), 0, a.s, a.src, a.B, a.nnz, a.loc, a.offsets, a.D, a.mode, a.out, a.hit_miss,
                        a.status);
     EMB_RETURN_IF_LAUNCH_FAILED();
     return EMB_OK;
 }
 
-template <int BITS>
+template <int FMT>
 int dispatch_staged_quant(int lpr, const StagedArgs &a)
 {
     switch (lpr) {
-        case 1: return launch_staged_quant<1, BITS>(a);
-        case 2: return launch_staged_quant<2, BITS>(a);
-        case 4: return launch_staged_quant<4, BITS>(a);
-        case 8: return launch_staged_quant<8, BITS>(a);
-        case 16: return launch_staged_quant<16, BITS>(a);
-        case 32: return launch_staged_quant<32, BITS>(a);
-        default: return launch_staged_quant<64, BITS>(a);
+        case 1: return launch_staged_quant<1, FMT>(a);
+        case 2: return launch_staged_quant<2, FMT>(a);
+        case 4: return launch_staged_quant<4, FMT>(a);
+        case 8: return launch_staged_quant<8, FMT>(a);
+        case 16: return launch_staged_quant<16, FMT>(a);
+        case 32: return launch_staged_quant<32, FMT>(a);
+        default: return launch_staged_quant<64, FMT>(a);
     }
 }
 
@@ -333,9 +333,14 @@ extern "C" int emb_bag_forward_staged(const void *table_dev, int64_t num_rows, i
     a.hit_miss = reinterpret_cast<unsigned long long *>(hit_miss_dev);
     a.status = status_dev;
     a.s = emb_stream(stream);
-    if (emb_is_quant(dtype))
-        return emb_quant_bits(dtype) == 8 ? dispatch_staged_quant<8>(emb_quant_lanes(D), a)
-                                          : dispatch_staged_quant<4>(emb_quant_lanes(D), a);
+    if (emb_is_quant(dtype)) {
+        const int ql = emb_quant_lanes(D);
+        switch (emb_quant_format(dtype)) {
+            case EMB_FMT_INT8: return dispatch_staged_quant<EMB_FMT_INT8>(ql, a);
+            case EMB_FMT_INT4: return dispatch_staged_quant<EMB_FMT_INT4>(ql, a);
+            default: return dispatch_staged_quant<EMB_FMT_MXFP4>(ql, a);
+        }
+    }
     int lpr, cpl;
     emb_row_split((int)(a.src.row_bytes / 16), lpr, cpl);
     const bool bf16 = dtype == EMB_BF16;

@@ -198,15 +198,18 @@ def run_step(w: Workload, tables: emb.TableSet, db: DeviceBatch, buf: StepBuffer
 class HotRowCache:
     """The HBM hot-row cache of one host-resident table together with the frequency-based policy that
     decides what it holds: two cache buffers (the lookups read one while a refresh fills the other),
-    one access counter per table row, and the selection workspace.  Call sequencing only."""
+    one access counter per table row, and the selection workspace.  ``cache_dtype`` (a quantised type, for
+    a table of fp32 or bf16 rows): the rows are quantised as they are written to the cache.  Call sequencing only."""
 
     def __init__(self, table_ptr: int, num_rows: int, D: int, dtype: str, num_hot: int, salt: int,
-                 device: torch.device, decay_shift: int = 1):
+                 device: torch.device, decay_shift: int = 1, cache_dtype: Optional[str] = None):
         self.table_ptr, self.R, self.D, self.dtype, self.salt = int(table_ptr), int(num_rows), int(D), dtype, int(salt)
         self.capacity, self.decay_shift = int(num_hot), int(decay_shift)
-        rowb = emb.emb_row_bytes(D, dtype)
-        shape = (self.capacity, rowb) if dtype in emb.QUANT_DTYPES else (self.capacity, D)
-        tdt = torch.uint8 if dtype in emb.QUANT_DTYPES else (torch.float32 if dtype == "f32" else torch.bfloat16)
+        self.cache_dtype = cache_dtype
+        stored = cache_dtype or dtype
+        rowb = emb.emb_row_bytes(D, stored)
+        shape = (self.capacity, rowb) if stored in emb.QUANT_DTYPES else (self.capacity, D)
+        tdt = torch.uint8 if stored in emb.QUANT_DTYPES else (torch.float32 if stored == "f32" else torch.bfloat16)
         self.rows = [torch.empty(shape, dtype=tdt, device=device) for _ in range(2)]
         self.index = [torch.empty(emb.emb_cache_index_bytes(num_rows), dtype=torch.uint8, device=device)
                       for _ in range(2)]
@@ -219,13 +222,20 @@ class HotRowCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.active = 0
         self.num_hot = 0                                             # starts empty: every lookup is a miss
-        emb.emb_cache_build(self.table_ptr, self.R, D, dtype, self.hot[:0], self.rows[0], self.index[0], self.status)
+        self._build(self.hot[:0], 0)
+
+    def _build(self, hot_rows: torch.Tensor, which: int) -> None:
+        if self.cache_dtype:
+            emb.emb_cache_build_quantized(self.table_ptr, self.R, self.D, self.dtype, self.cache_dtype, hot_rows,
+                                          self.rows[which], self.index[which], self.status)
+        else:
+            emb.emb_cache_build(self.table_ptr, self.R, self.D, self.dtype, hot_rows, self.rows[which], self.index[which],
+                                self.status)
 
     def set_static(self, hot_rows: torch.Tensor) -> None:
         """Load a given hot set (ascending rows) into the active buffers."""
         self.num_hot = hot_rows.numel()
-        emb.emb_cache_build(self.table_ptr, self.R, self.D, self.dtype, hot_rows, self.rows[self.active],
-                            self.index[self.active], self.status)
+        self._build(hot_rows, self.active)
 
     def observe(self, raw: torch.Tensor) -> None:
         emb.emb_cache_observe_hashed(self.R, self.salt, raw, self.freq, self.status)
@@ -234,12 +244,23 @@ class HotRowCache:
         """Select the most frequently looked-up rows and fill the idle buffers with them, taking the rows the
         active cache already holds from HBM; then swap.  In stream order with the lookups."""
         new = 1 - self.active
-        emb.emb_cache_refresh(self.freq, self.capacity, self.decay_shift, self.workspace, self.table_ptr, self.D,
-                              self.dtype, self.rows[self.active], self.index[self.active], self.num_hot, self.hot,
-                              self.rows[new], self.index[new], self.moved, self.info, self.status)
+        if self.cache_dtype:
+            emb.emb_cache_select(self.freq, self.capacity, self.decay_shift, self.workspace, self.hot, self.info)
+            emb.emb_cache_rebuild_quantized(self.table_ptr, self.R, self.D, self.dtype, self.cache_dtype,
+                                            self.rows[self.active], self.index[self.active], self.num_hot,
+                                            self.hot[:self.capacity], self.rows[new], self.index[new], self.moved, self.status)
+        else:
+            emb.emb_cache_refresh(self.freq, self.capacity, self.decay_shift, self.workspace, self.table_ptr, self.D,
+                                  self.dtype, self.rows[self.active], self.index[self.active], self.num_hot, self.hot,
+                                  self.rows[new], self.index[new], self.moved, self.info, self.status)
         self.active, self.num_hot = new, self.capacity
 
     def forward_hashed(self, raw: torch.Tensor, offsets: torch.Tensor, B: int, mode: str, out: torch.Tensor) -> None:
+        if self.cache_dtype:
+            emb.emb_bag_forward_cached_quantized_hashed(self.table_ptr, self.R, self.D, self.dtype, self.cache_dtype,
+                                                        self.rows[self.active], self.index[self.active], self.num_hot, self.salt,
+                                                        raw, offsets, B, mode, out, self.hit_miss, self.status)
+            return
         emb.emb_bag_forward_cached_hashed(self.table_ptr, self.R, self.D, self.dtype, self.rows[self.active],
                                           self.index[self.active], self.num_hot, self.salt, raw, offsets, B, mode, out,
                                           self.hit_miss, self.status)
@@ -251,6 +272,7 @@ class HostedTableSet:
 
     def __init__(self, caches: List[HotRowCache], device: torch.device):
         assert len({(c.D, c.dtype) for c in caches}) == 1, "the tables of one launch share D and storage type"
+        assert not any(c.cache_dtype for c in caches), "caches of the tables' own storage type"
         self.caches, self.device = list(caches), device
         self.D, self.dtype = caches[0].D, caches[0].dtype
         self.hit_miss = torch.zeros(2, dtype=torch.int64, device=device)
