@@ -22,6 +22,7 @@ typedef float mx_f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 mx_b8 __attribute__((ext_vector_type(8)));
 typedef float mx_f4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 mx_b4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef __bf16 mx_b8_any __attribute__((ext_vector_type(8), aligned(2)));
 
 enum { X_MXFP4 = 0, X_BF16 = 1, X_F32 = 2 };
 
@@ -41,6 +42,40 @@ __device__ __forceinline__ mx_i8 mx_operand(const uint4 &v)
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int j) { return j == 0 ? v.x : (j == 1 ? v.y : (j == 2 ? v.z : v.w)); }
+
+// 16 neighbouring elements of a row of the output, v[0] the first four.
+template <bool OUT_BF16>
+__device__ __forceinline__ void store_16(char *out, int64_t row, int64_t n, int64_t N, const mx_f4 (&v)[4])
+{
+    if constexpr (OUT_BF16) {
+        __bf16 *o = reinterpret_cast<__bf16 *>(out) + row + n;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            mx_b8_any b;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) b[k] = (__bf16)v[2 * h + k / 4][k % 4];
+            if (n + 8 * h + 8 <= N) {
+                *reinterpret_cast<mx_b8_any *>(o + 8 * h) = b;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (n + 8 * h + k < N) o[8 * h + k] = b[k];
+            }
+        }
+    } else {
+        float *o = reinterpret_cast<float *>(out) + row + n;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (n + 4 * t + 4 <= N) {
+                *reinterpret_cast<mx_f4_any *>(o + 4 * t) = v[t];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (n + 4 * t + k < N) o[4 * t + k] = v[t][k];
+            }
+        }
+    }
+}
 
 // 8 codes of one word, by their block's power of two, as bf16 (exact)
 __device__ __forceinline__ mx_b8 codes_to_bf16(uint32_t w, float scale)
@@ -238,6 +273,223 @@ int launch_direct(ProductArgs a, hipStream_t s)
     return EMB_OK;
 }
 
+// ---------------------------------------------------------------------------
+// tiles in LDS
+// ---------------------------------------------------------------------------
+// Both operands MXFP4: a workgroup makes a tile of 256 x 256 (8 wavefronts of 128 x 64) or, where those would not fill the
+// chip, 128 x 128 (4 of 64 x 64), from stages of 256 elements that go straight to LDS, two buffers in turn.  A wavefront
+// reads LDS 12 times for 32 MFMA of 16 cycles: LDS is busy 3/8 of the time, the matrix unit is what bounds it, and what keeps
+// it from its rate is the wait at a stage's end.  8192 x 8192 x 4096, us: chunks of the next stage requested ahead of
+// the products 209, one at a time between groups of them 177 (3.1 PFLOP/s; no requests at all: 145).
+#define EMB_LDS __attribute__((address_space(3)))
+typedef uint32_t mx_u4 __attribute__((ext_vector_type(4)));
+
+// 256 elements of a row are 8 chunks of 16 bytes; a tile keeps them in 128 bytes a row, chunk c at place c ^ key(row), where
+// the key makes the 16 rows that a quarter of a wavefront reads at once lie in 16 different places of 256 bytes.
+// W's tiles of the matrix unit take rows 16 * (i / 4) + 4 * t + i % 4 (i: the unit's row, t: tile), so that a lane's four
+// tiles end as 16 neighbouring n; x's take 16 neighbouring rows.
+__device__ __forceinline__ int key_x(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int key_w(int row) { return ((row >> 1) & 1) | ((row >> 3) & 6); }
+
+constexpr int STAGE_CHUNKS = 8;
+
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// One operand's rows of a tile, seen as a buffer that begins with the tile's first row: 32-bit offsets, the stage's in a scalar,
+// and what lies beyond its end reads as zero, which is where the chunks are sent that the last stage does not have.
+constexpr uint32_t BUFFER_END = 1u << 30, BEYOND = 1u << 31;    // (a tile's rows end below: 256 rows of at most 34816 bytes)
+
+template <int ROWS, int THREADS, bool IS_W>
+struct StageOperand {
+    static constexpr int LOADS = ROWS * STAGE_CHUNKS / THREADS;
+    __amdgpu_buffer_rsrc_t rows;
+    uint32_t off[LOADS];       // of this thread's chunk of row u * THREADS / 8 + threadIdx / 8
+    __device__ __forceinline__ static int chunk(int u)
+    {
+        const int row = u * (THREADS / STAGE_CHUNKS) + threadIdx.x / STAGE_CHUNKS;
+        return (threadIdx.x % STAGE_CHUNKS) ^ (IS_W ? key_w(row) : key_x(row));
+    }
+    // have: how many rows there are (the others repeat the last)
+    __device__ __forceinline__ void init(const char *base, int64_t have, int64_t pitch)
+    {
+        rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, BUFFER_END, 0x00020000);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int row = u * (THREADS / STAGE_CHUNKS) + threadIdx.x / STAGE_CHUNKS;
+            off[u] = __umul24((uint32_t)(row < have ? row : (int)have - 1), (uint32_t)pitch) + 16u * (uint32_t)chunk(u);
+        }
+    }
+    // Chunks of a stage straight to LDS; the row still has `valid` of them.
+    __device__ __forceinline__ void load(int u, int stage, char *lds, int valid) const
+    {
+        const uint32_t at = chunk(u) < valid ? off[u] : BEYOND;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (EMB_LDS void *)(lds + (u * THREADS + (threadIdx.x & ~63u)) * 16), 16, (int)at,
+                                                 stage * (STAGE_CHUNKS * 16), 0, 0);
+    }
+};
+
+// ONE: D is at most 128.
+template <int WM, int WN, int MT, bool ONE, bool OUT_BF16>
+__global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs a)
+{
+    constexpr int NT = 4, THREADS = 64 * WM * WN, BM = WM * MT * 16, BN = WN * 64;
+    static_assert(BM + BN == THREADS, "a thread fetches one row's scales");
+    __shared__ __attribute__((aligned(16))) char x0[BM * 128], x1[BM * 128], w0[BN * 128], w1[BN * 128];
+    __shared__ uint2 s0[THREADS], s1[THREADS];        // scale bytes of the stage: x's rows, then W's
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+    const int wm = wave % WM, wn = wave / WM;
+    // Tiles of a die's share: groups of up to 8 rows of tiles, column by column.  (The quotients come from the vector unit:
+    // told to be uniform, so that addresses stay scalar bases and 32-bit offsets.)
+    const uint32_t tile = emb_xcd_block(blockIdx.x, gridDim.x), tiles_m = (uint32_t)a.tiles_m, tiles_n = (uint32_t)a.tiles_n;
+    if (tile >= tiles_m * tiles_n) return;            // uniform
+    const uint32_t group = uniform(tile / (8 * tiles_n)), in_group = tile - group * 8 * tiles_n;
+    const uint32_t high = tiles_m - group * 8 < 8 ? tiles_m - group * 8 : 8;
+    const uint32_t tn = uniform(in_group / high), tm = group * 8 + in_group - tn * high;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const char *xbase = a.x + m0 * a.x_pitch, *wbase = a.w + n0 * a.w_pitch;
+    const int64_t xrows = a.M - m0, wrows = a.N - n0;
+    const int nb = a.D / 32, stages = (nb + STAGE_CHUNKS - 1) / STAGE_CHUNKS, last = nb - (stages - 1) * STAGE_CHUNKS;
+
+    StageOperand<BM, THREADS, false> xo;
+    StageOperand<BN, THREADS, true> wo;
+    xo.init(xbase, xrows < BM ? xrows : BM, a.x_pitch);
+    wo.init(wbase, wrows < BN ? wrows : BN, a.w_pitch);
+    const char *srow;                                 // the scales that this thread fetches
+    {
+        const int64_t have = tid < BM ? xrows : wrows;
+        int64_t row = tid < BM ? tid : tid - BM;
+        if (row >= have) row = have - 1;
+        srow = (tid < BM ? xbase + row * a.x_pitch : wbase + row * a.w_pitch) + a.D / 2;
+    }
+    // the lane's first row in either tile; its others lie 16 rows (x) and 4 rows (W) on, with the same key
+    const int xrow0 = wm * MT * 16 + r, wrow0 = wn * 64 + 16 * (r >> 2) + (r & 3);
+    const int xkey = key_x(xrow0), wkey = key_w(wrow0);
+    uint2 sc;
+    mx_f4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = mx_f4{0.f, 0.f, 0.f, 0.f};
+
+    // (A stage past the last one reads nothing: the loop below stays one block of instructions, out of which the compiler
+    // moves no MFMA.)
+    auto fetch_scales = [&](int st) { sc = load_u2(srow + (st < stages ? st : stages - 1) * STAGE_CHUNKS); };
+    auto fetch_part = [&](int part, int st, char *xl, char *wl) {
+        if (part < xo.LOADS) xo.load(part, st, xl, nb - st * STAGE_CHUNKS);
+        else wo.load(part - xo.LOADS, st, wl, nb - st * STAGE_CHUNKS);
+    };
+    constexpr int PARTS = (BM + BN) * STAGE_CHUNKS / THREADS;
+    auto fetch = [&](int st, char *xl, char *wl) {
+        fetch_scales(st);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) fetch_part(k, st, xl, wl);
+    };
+    auto ready = [&](int st, uint2 *sl) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this thread's chunks of the stage are in LDS
+        uint2 v = sc;
+        if (st + 1 == stages && last < STAGE_CHUNKS) {   // blocks past the row: a scale that is a number
+            const uint64_t keep = (1ull << (8 * last)) - 1, all = (((uint64_t)v.y << 32 | v.x) & keep) | (0x7F7F7F7F7F7F7F7Full & ~keep);
+            v = make_uint2((uint32_t)all, (uint32_t)(all >> 32));
+        }
+        sl[tid] = v;
+        __syncthreads();                              // everyone's are, and nobody reads the other buffer any more
+    };
+    // One stage is two steps of the matrix unit: lane group g takes chunk 2g, then 2g + 1.  Rows of at most 4 chunks are one
+    // step: group g takes chunk g.
+    auto compute = [&](const char *xl, const char *wl, const uint2 *sl, int next, char *xnext, char *wnext) {
+        constexpr bool HALF = ONE;
+        const char *sx = reinterpret_cast<const char *>(sl) + xrow0 * 8, *sw = reinterpret_cast<const char *>(sl) + (BM + wrow0) * 8;
+        int xs[MT], ws[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xs[i] = HALF ? (int)(uint8_t)sx[i * 128 + g] : (int)*reinterpret_cast<const uint16_t *>(sx + i * 128 + 2 * g);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) ws[t] = HALF ? (int)(uint8_t)sw[t * 32 + g] : (int)*reinterpret_cast<const uint16_t *>(sw + t * 32 + 2 * g);
+        // Reads run one group of MFMA ahead: 2 of x's tiles by 4 of W's, 128 cycles of the matrix unit.
+        constexpr int XG = 2, PER_STEP = MT / XG, GROUPS = PER_STEP * (HALF ? 1 : 2);
+        mx_u4 xv[2][XG], wv[2][NT];
+        auto read_w = [&](int step) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                wv[step][t] = *reinterpret_cast<const mx_u4 *>(wl + wrow0 * 128 + (((HALF ? g : 2 * g + step) ^ wkey) * 16) + t * 512);
+        };
+        auto read_x = [&](int q) {
+#pragma unroll
+            for (int i = 0; i < XG; ++i)
+                xv[q & 1][i] = *reinterpret_cast<const mx_u4 *>(xl + xrow0 * 128 + (((HALF ? g : 2 * g + q / PER_STEP) ^ xkey) * 16) +
+                                                                ((q % PER_STEP) * XG + i) * 2048);
+        };
+        read_w(0);
+        read_x(0);
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) {
+            const int step = q / PER_STEP, i0 = (q % PER_STEP) * XG;
+            if (!HALF && q == 0) read_w(1);
+            if (q + 1 < GROUPS) read_x(q + 1);
+            if (!HALF) {                              // the next stage's chunks, spread over this one's products
+                if (q == 0) fetch_scales(next);
+#pragma unroll
+                for (int k = q * PARTS / GROUPS; k < (q + 1) * PARTS / GROUPS; ++k) fetch_part(k, next, xnext, wnext);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < XG; ++i)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const mx_u4 w = wv[step][t], x = xv[q & 1][i];
+                    const mx_i8 wa = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+                    const mx_i8 xa = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
+                    if (step == 0)
+                        acc[i0 + i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xa, acc[i0 + i][t], 4, 4, 0, ws[t], 0, xs[i0 + i]);
+                    else
+                        acc[i0 + i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xa, acc[i0 + i][t], 4, 4, 1, ws[t], 1, xs[i0 + i]);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if constexpr (ONE) {
+        fetch(0, x0, w0);
+        ready(0, s0);
+        compute(x0, w0, s0, 0, x0, w0);
+    } else {
+        // Two buffers, of different names so that the compiler sees that what is fetched into one is not read from the other.
+        int st = 0;
+        if (stages & 1) {
+            fetch(0, x1, w1);
+            ready(0, s1);
+            compute(x1, w1, s1, 1, x0, w0);
+            st = 1;
+        } else {
+            fetch(0, x0, w0);
+        }
+        for (; st < stages; st += 2) {
+            ready(st, s0);
+            compute(x0, w0, s0, st + 1, x1, w1);
+            ready(st + 1, s1);
+            compute(x1, w1, s1, st + 2, x0, w0);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0F70);           // nothing is on its way to LDS when the workgroup ends
+    }
+
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + wm * MT * 16 + 16 * i + r, n = n0 + wn * 64 + 16 * g;
+        if (m >= a.M) continue;
+        store_16<OUT_BF16>(a.out, m * a.out_stride, n, a.N, acc[i]);
+    }
+}
+
+template <int WM, int WN, int MT, bool ONE, bool OUT_BF16>
+int launch_tiled(ProductArgs a, hipStream_t s)
+{
+    constexpr int BM = WM * MT * 16, BN = WN * 64;
+    a.tiles_m = (a.M + BM - 1) / BM;
+    a.tiles_n = (a.N + BN - 1) / BN;
+    if (a.tiles_n > (int64_t)0x7FFFFF00 / a.tiles_m) return EMB_ERR_UNSUPPORTED;
+    const int64_t blocks = emb_round_up_xcds(a.tiles_m * a.tiles_n);
+    hipLaunchKernelGGL((product_tiled_kernel<WM, WN, MT, ONE, OUT_BF16>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, a);
+    return EMB_OK;
+}
+
 template <int XT, bool OUT_BF16>
 int dispatch_product(const ProductArgs &a, hipStream_t s)
 {
@@ -248,6 +500,11 @@ int dispatch_product(const ProductArgs &a, hipStream_t s)
         return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
     }
     if (a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
+    if constexpr (XT == X_MXFP4) {
+        if (a.D <= 128) return launch_tiled<2, 2, 4, true, OUT_BF16>(a, s);
+        if ((a.M + 255) / 256 * ((a.N + 255) / 256) >= 256) return launch_tiled<2, 4, 8, false, OUT_BF16>(a, s);
+        return launch_tiled<2, 2, 4, false, OUT_BF16>(a, s);
+    }
     return launch_direct<XT, 4, 4, 1, OUT_BF16>(a, s);
 }
 
