@@ -34,6 +34,7 @@ struct ProductArgs {
     char *out;
     int64_t out_stride;            // elements
     int64_t tiles_m, tiles_n;      // workgroup tiles
+    uint32_t die_rows;             // rows of dies that share them: 1, 2, 4 or 8
 };
 
 __device__ __forceinline__ mx_i8 mx_operand(const uint4 &v)
@@ -43,14 +44,14 @@ __device__ __forceinline__ mx_i8 mx_operand(const uint4 &v)
 
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int j) { return j == 0 ? v.x : (j == 1 ? v.y : (j == 2 ? v.z : v.w)); }
 
-// 16 neighbouring elements of a row of the output, v[0] the first four.
-template <bool OUT_BF16>
-__device__ __forceinline__ void store_16(char *out, int64_t row, int64_t n, int64_t N, const mx_f4 (&v)[4])
+// 4 * V neighbouring elements of a row of the output, v[0] the first four.
+template <int V, bool OUT_BF16>
+__device__ __forceinline__ void store_run(char *out, int64_t row, int64_t n, int64_t N, const mx_f4 (&v)[V])
 {
     if constexpr (OUT_BF16) {
         __bf16 *o = reinterpret_cast<__bf16 *>(out) + row + n;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < V / 2; ++h) {
             mx_b8_any b;
 #pragma unroll
             for (int k = 0; k < 8; ++k) b[k] = (__bf16)v[2 * h + k / 4][k % 4];
@@ -65,7 +66,7 @@ __device__ __forceinline__ void store_16(char *out, int64_t row, int64_t n, int6
     } else {
         float *o = reinterpret_cast<float *>(out) + row + n;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < V; ++t) {
             if (n + 4 * t + 4 <= N) {
                 *reinterpret_cast<mx_f4_any *>(o + 4 * t) = v[t];
             } else {
@@ -284,8 +285,9 @@ int launch_direct(ProductArgs a, hipStream_t s)
 #define EMB_LDS __attribute__((address_space(3)))
 typedef uint32_t mx_u4 __attribute__((ext_vector_type(4)));
 
-// 256 elements of a row are 8 chunks of 16 bytes; a tile keeps them in 128 bytes a row, chunk c at place c ^ key(row), where
-// the key makes the 16 rows that a quarter of a wavefront reads at once lie in 16 different places of 256 bytes.
+// 256 elements of a row are 8 chunks of 16 bytes; a tile keeps them in 128 bytes a row, chunk c at place c ^ key(row).  LDS
+// serves a 16-byte read 16 lanes at a time, of which 8 are of one lane group (rows 0-3 and 12-15 of a tile, or 4-11) and 8 of
+// its neighbour (the other rows): groups that read neighbouring chunks then find 16 different places of 256 bytes.
 // W's tiles of the matrix unit take rows 16 * (i / 4) + 4 * t + i % 4 (i: the unit's row, t: tile), so that a lane's four
 // tiles end as 16 neighbouring n; x's take 16 neighbouring rows.
 __device__ __forceinline__ int key_x(int row) { return (row >> 1) & 7; }
@@ -295,9 +297,27 @@ constexpr int STAGE_CHUNKS = 8;
 
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
+// The tile of a workgroup, if it has one.  The dies share the tiles as a grid of die_rows x 8 / die_rows, so that a die's L2 holds
+// few panels of either operand; within its part a die goes row by row through strips of 8 columns.  (The quotients come from
+// the vector unit: told to be uniform, so that addresses are scalar bases and 32-bit offsets.)
+__device__ __forceinline__ bool tile_of(const ProductArgs &a, uint32_t &tm, uint32_t &tn)
+{
+    const uint32_t die = blockIdx.x % EMB_XCDS, i = blockIdx.x / EMB_XCDS, tiles_m = (uint32_t)a.tiles_m, tiles_n = (uint32_t)a.tiles_n;
+    const uint32_t die_cols = EMB_XCDS / a.die_rows, high = uniform((tiles_m + a.die_rows - 1) / a.die_rows),
+                   wide = uniform((tiles_n + die_cols - 1) / die_cols);
+    const uint32_t row0 = die % a.die_rows * high, col0 = die / a.die_rows * wide;
+    const uint32_t strip = uniform(i / (8 * high)), in_strip = i - strip * 8 * high;
+    const uint32_t columns = wide - strip * 8 < 8 ? wide - strip * 8 : 8;
+    const uint32_t row = uniform(in_strip / columns);
+    tm = row0 + row;
+    tn = col0 + strip * 8 + in_strip - row * columns;
+    return tm < tiles_m && tn < tiles_n;
+}
+
 // One operand's rows of a tile, seen as a buffer that begins with the tile's first row: 32-bit offsets, the stage's in a scalar,
 // and what lies beyond its end reads as zero, which is where the chunks are sent that the last stage does not have.
-constexpr uint32_t BUFFER_END = 1u << 30, BEYOND = 1u << 31;    // (a tile's rows end below: 256 rows of at most 34816 bytes)
+constexpr uint32_t BUFFER_END = 1u << 30, BEYOND = 1u << 31;
+constexpr int64_t MOST_PITCH = 1 << 22;    // of rows of x that are tiled: 128 of them end below BUFFER_END, as 256 MXFP4 rows do (34816 bytes)
 
 template <int ROWS, int THREADS, bool IS_W>
 struct StageOperand {
@@ -335,16 +355,11 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
     constexpr int NT = 4, THREADS = 64 * WM * WN, BM = WM * MT * 16, BN = WN * 64;
     static_assert(BM + BN == THREADS, "a thread fetches one row's scales");
     __shared__ __attribute__((aligned(16))) char x0[BM * 128], x1[BM * 128], w0[BN * 128], w1[BN * 128];
-    __shared__ uint2 s0[THREADS], s1[THREADS];        // scale bytes of the stage: x's rows, then W's
+    __shared__ __attribute__((aligned(16))) uint16_t s0[THREADS * 4], s1[THREADS * 4];   // scales of a stage: x's rows, then W's
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
     const int wm = wave % WM, wn = wave / WM;
-    // Tiles of a die's share: groups of up to 8 rows of tiles, column by column.  (The quotients come from the vector unit:
-    // told to be uniform, so that addresses stay scalar bases and 32-bit offsets.)
-    const uint32_t tile = emb_xcd_block(blockIdx.x, gridDim.x), tiles_m = (uint32_t)a.tiles_m, tiles_n = (uint32_t)a.tiles_n;
-    if (tile >= tiles_m * tiles_n) return;            // uniform
-    const uint32_t group = uniform(tile / (8 * tiles_n)), in_group = tile - group * 8 * tiles_n;
-    const uint32_t high = tiles_m - group * 8 < 8 ? tiles_m - group * 8 : 8;
-    const uint32_t tn = uniform(in_group / high), tm = group * 8 + in_group - tn * high;
+    uint32_t tm, tn;
+    if (!tile_of(a, tm, tn)) return;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const char *xbase = a.x + m0 * a.x_pitch, *wbase = a.w + n0 * a.w_pitch;
     const int64_t xrows = a.M - m0, wrows = a.N - n0;
@@ -384,38 +399,52 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
 #pragma unroll
         for (int k = 0; k < PARTS; ++k) fetch_part(k, st, xl, wl);
     };
-    auto ready = [&](int st, uint2 *sl) {
+    // Scales in LDS: 16 bytes for a pair of the unit's tiles and a row of them, 4 for each lane group: its two blocks in the
+    // first tile, then in the second.  One read gives a lane the scales of two tiles and both steps.
+    int splace;
+    {
+        const int row = tid < BM ? tid : tid - BM;
+        const int in_tile = tid < BM ? row & 15 : ((row >> 2) & 12) | (row & 3), t = tid < BM ? row >> 4 : (row >> 6) * 4 + ((row >> 2) & 3);
+        splace = (tid < BM ? 0 : BM * 4) + ((t >> 1) * 16 + in_tile) * 8 + (t & 1);
+    }
+    auto ready = [&](int st, uint16_t *sl) {
         __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this thread's chunks of the stage are in LDS
-        uint2 v = sc;
+        uint64_t v = (uint64_t)sc.y << 32 | sc.x;
         if (st + 1 == stages && last < STAGE_CHUNKS) {   // blocks past the row: a scale that is a number
-            const uint64_t keep = (1ull << (8 * last)) - 1, all = (((uint64_t)v.y << 32 | v.x) & keep) | (0x7F7F7F7F7F7F7F7Full & ~keep);
-            v = make_uint2((uint32_t)all, (uint32_t)(all >> 32));
+            const uint64_t keep = (1ull << (8 * last)) - 1;
+            v = (v & keep) | (0x7F7F7F7F7F7F7F7Full & ~keep);
         }
-        sl[tid] = v;
+        const uint32_t lo = __builtin_amdgcn_perm((uint32_t)(v >> 32), (uint32_t)v, 0x05010400u),   // bytes 0 4 1 5
+                       hi = __builtin_amdgcn_perm((uint32_t)(v >> 32), (uint32_t)v, 0x07030602u);   // 2 6 3 7
+        sl[splace] = (uint16_t)lo;
+        sl[splace + 2] = (uint16_t)(lo >> 16);
+        sl[splace + 4] = (uint16_t)hi;
+        sl[splace + 6] = (uint16_t)(hi >> 16);
         __syncthreads();                              // everyone's are, and nobody reads the other buffer any more
     };
-    // One stage is two steps of the matrix unit: lane group g takes chunk 2g, then 2g + 1.  Rows of at most 4 chunks are one
-    // step: group g takes chunk g.
-    auto compute = [&](const char *xl, const char *wl, const uint2 *sl, int next, char *xnext, char *wnext) {
+    // One stage is two steps of the matrix unit: lane group g takes chunk g, then 4 + g, whose scale bytes lie side by side in
+    // LDS.  Rows of at most 4 chunks are one step.
+    auto compute = [&](const char *xl, const char *wl, const uint16_t *sl, int next, char *xnext, char *wnext) {
         constexpr bool HALF = ONE;
-        const char *sx = reinterpret_cast<const char *>(sl) + xrow0 * 8, *sw = reinterpret_cast<const char *>(sl) + (BM + wrow0) * 8;
-        int xs[MT], ws[NT];
+        const char *sx = reinterpret_cast<const char *>(sl) + (wm * (MT / 2) * 16 + r) * 16 + g * 4;
+        const char *sw = reinterpret_cast<const char *>(sl) + BM * 8 + (wn * (NT / 2) * 16 + r) * 16 + g * 4;
+        int xs[MT / 2], ws[NT / 2];                   // bytes: first tile, step 0 and 1; second tile
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xs[i] = HALF ? (int)(uint8_t)sx[i * 128 + g] : (int)*reinterpret_cast<const uint16_t *>(sx + i * 128 + 2 * g);
+        for (int i = 0; i < MT / 2; ++i) xs[i] = *reinterpret_cast<const int *>(sx + i * 256);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) ws[t] = HALF ? (int)(uint8_t)sw[t * 32 + g] : (int)*reinterpret_cast<const uint16_t *>(sw + t * 32 + 2 * g);
+        for (int t = 0; t < NT / 2; ++t) ws[t] = *reinterpret_cast<const int *>(sw + t * 256);
         // Reads run one group of MFMA ahead: 2 of x's tiles by 4 of W's, 128 cycles of the matrix unit.
         constexpr int XG = 2, PER_STEP = MT / XG, GROUPS = PER_STEP * (HALF ? 1 : 2);
         mx_u4 xv[2][XG], wv[2][NT];
         auto read_w = [&](int step) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                wv[step][t] = *reinterpret_cast<const mx_u4 *>(wl + wrow0 * 128 + (((HALF ? g : 2 * g + step) ^ wkey) * 16) + t * 512);
+                wv[step][t] = *reinterpret_cast<const mx_u4 *>(wl + wrow0 * 128 + (((4 * step + g) ^ wkey) * 16) + t * 512);
         };
         auto read_x = [&](int q) {
 #pragma unroll
             for (int i = 0; i < XG; ++i)
-                xv[q & 1][i] = *reinterpret_cast<const mx_u4 *>(xl + xrow0 * 128 + (((HALF ? g : 2 * g + q / PER_STEP) ^ xkey) * 16) +
+                xv[q & 1][i] = *reinterpret_cast<const mx_u4 *>(xl + xrow0 * 128 + (((4 * (q / PER_STEP) + g) ^ xkey) * 16) +
                                                                 ((q % PER_STEP) * XG + i) * 2048);
         };
         read_w(0);
@@ -438,10 +467,16 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
                     const mx_u4 w = wv[step][t], x = xv[q & 1][i];
                     const mx_i8 wa = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
                     const mx_i8 xa = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
-                    if (step == 0)
-                        acc[i0 + i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xa, acc[i0 + i][t], 4, 4, 0, ws[t], 0, xs[i0 + i]);
-                    else
-                        acc[i0 + i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xa, acc[i0 + i][t], 4, 4, 1, ws[t], 1, xs[i0 + i]);
+#define EMB_MFMA(WB, XB)                                                                                                    \
+    acc[i0 + i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xa, acc[i0 + i][t], 4, 4, WB, ws[t / 2], XB, xs[(i0 + i) / 2])
+                    if (step == 0) {
+                        if (t % 2 == 0) { if (i % 2 == 0) EMB_MFMA(0, 0); else EMB_MFMA(0, 2); }
+                        else { if (i % 2 == 0) EMB_MFMA(2, 0); else EMB_MFMA(2, 2); }
+                    } else {
+                        if (t % 2 == 0) { if (i % 2 == 0) EMB_MFMA(1, 1); else EMB_MFMA(1, 3); }
+                        else { if (i % 2 == 0) EMB_MFMA(3, 1); else EMB_MFMA(3, 3); }
+                    }
+#undef EMB_MFMA
                 }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -474,19 +509,230 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
     for (int i = 0; i < MT; ++i) {
         const int64_t m = m0 + wm * MT * 16 + 16 * i + r, n = n0 + wn * 64 + 16 * g;
         if (m >= a.M) continue;
-        store_16<OUT_BF16>(a.out, m * a.out_stride, n, a.N, acc[i]);
+        store_run<NT, OUT_BF16>(a.out, m * a.out_stride, n, a.N, acc[i]);
     }
+}
+
+// The dies' part of the tiles: of the four ways to share them the one whose largest part is smallest, of equals the one with
+// the fewest rows and columns in a part.  Returns the workgroups of the launch.
+inline int64_t share_tiles(ProductArgs &a, int64_t bm, int64_t bn)
+{
+    a.tiles_m = (a.M + bm - 1) / bm;
+    a.tiles_n = (a.N + bn - 1) / bn;
+    int64_t best = INT64_MAX, around = 0;
+    for (uint32_t rows = 1; rows <= EMB_XCDS; rows *= 2) {
+        const int64_t high = (a.tiles_m + rows - 1) / rows, wide = (a.tiles_n + EMB_XCDS / rows - 1) / (EMB_XCDS / rows);
+        if (high * wide < best || (high * wide == best && high + wide < around)) {
+            best = high * wide;
+            around = high + wide;
+            a.die_rows = rows;
+        }
+    }
+    return best * EMB_XCDS;
 }
 
 template <int WM, int WN, int MT, bool ONE, bool OUT_BF16>
 int launch_tiled(ProductArgs a, hipStream_t s)
 {
-    constexpr int BM = WM * MT * 16, BN = WN * 64;
-    a.tiles_m = (a.M + BM - 1) / BM;
-    a.tiles_n = (a.N + BN - 1) / BN;
-    if (a.tiles_n > (int64_t)0x7FFFFF00 / a.tiles_m) return EMB_ERR_UNSUPPORTED;
-    const int64_t blocks = emb_round_up_xcds(a.tiles_m * a.tiles_n);
+    const int64_t blocks = share_tiles(a, WM * MT * 16, WN * 64);
+    if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((product_tiled_kernel<WM, WN, MT, ONE, OUT_BF16>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, a);
+    return EMB_OK;
+}
+
+// x in bf16 or fp32: W's codes become bf16 in registers.  A stage is 256 bytes of a row of x (128 bf16 or 64 fp32 elements) and
+// the 64 (32) bytes of codes that belong to them; scale bytes come from the row into a register, a stage ahead.  Lane group g
+// takes the stage's elements from g * STAGE / 4 on, in steps of 8: chunk c of a row of x stands at place c ^ wide_key_x(row).
+// Tiles are 128 x 128.  bf16: by wavefronts of 128 x 32, so that W's codes are widened once; two workgroups fill a CU's LDS
+// exactly.  fp32: by wavefronts of 32 x 128, so that every element of x is split into its three parts once.
+// W's rows stand in LDS in the order in which the unit's tiles take them: place 16 * (N * j + t) + 4 * a + b holds row
+// 16 * N * j + 4 * (N * a + t) + b, so that a lane's N tiles end as 4 * N neighbouring n (N = 2 or 4).
+// Keys for rows of 256 bytes, chunks 4 apart in neighbouring lane groups, and of 64 bytes, chunks 1 apart.
+__device__ __forceinline__ int wide_key_x(int row) { return (row & 3) | ((row >> 1) & 4) | (((row << 1) ^ row) & 8); }
+__device__ __forceinline__ int wide_key_w(int row) { return ((row >> 1) & 2) ^ ((row >> 3) & 1) * 3; }
+template <int N>
+__device__ __forceinline__ int w_row_at(int place)
+{
+    if (N == 2) return (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3);
+    return (place & ~63) | ((place & 12) << 2) | ((place & 48) >> 2) | (place & 3);
+}
+
+template <int XT, bool OUT_BF16>
+__global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
+{
+    constexpr bool F32 = XT == X_F32;
+    constexpr int STAGE = F32 ? 64 : 128, WM = F32 ? 4 : 1, WN = F32 ? 1 : 4, MT = F32 ? 2 : 8, NT = F32 ? 8 : 2, NG = F32 ? 4 : 2;
+    constexpr int BM = WM * MT * 16, BN = WN * NT * 16, THREADS = 256;
+    constexpr int XC = 16, WC = STAGE / 32;                       // 16-byte chunks of a row in a stage
+    constexpr int XL = BM * XC / THREADS, WL = BN * WC / THREADS; // that a thread fetches
+    constexpr int STEPS = STAGE / 32, KPARTS = F32 ? 3 : 1;
+    __shared__ __attribute__((aligned(16))) char x0[BM * 256], x1[BM * 256], w0[BN * WC * 16], w1[BN * WC * 16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+    const int wm = wave % WM, wn = wave / WM;
+    uint32_t tm, tn;
+    if (!tile_of(a, tm, tn)) return;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int xhave = a.M - m0 < BM ? (int)(a.M - m0) : BM, whave = a.N - n0 < BN ? (int)(a.N - n0) : BN;
+    const int nb = a.D / 32, stages = (a.D + STAGE - 1) / STAGE;
+    const __amdgpu_buffer_rsrc_t xrows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(a.x + m0 * a.x_pitch), 0, BUFFER_END, 0x00020000);
+    const __amdgpu_buffer_rsrc_t wrows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(a.w + n0 * a.w_pitch), 0, BUFFER_END, 0x00020000);
+
+    uint32_t xoff[XL], woff[WL], soff[NT];
+    const int xchunk = (tid % XC) ^ wide_key_x(tid / XC);            // (every row of this thread has the same place)
+    auto wchunk = [&](int u) {
+        const int place = (u * THREADS + tid) / WC;
+        return (tid % WC) ^ (F32 ? (place >> 3) & 1 : wide_key_w(place));
+    };
+#pragma unroll
+    for (int u = 0; u < XL; ++u) {
+        const int row = u * (THREADS / XC) + tid / XC;
+        xoff[u] = (uint32_t)(row < xhave ? row : xhave - 1) * (uint32_t)a.x_pitch + 16u * (uint32_t)xchunk;
+    }
+#pragma unroll
+    for (int u = 0; u < WL; ++u) {
+        const int row = w_row_at<NG>((u * THREADS + tid) / WC);
+        woff[u] = __umul24((uint32_t)(row < whave ? row : whave - 1), (uint32_t)a.w_pitch) + 16u * (uint32_t)wchunk(u);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = w_row_at<NG>(wn * NT * 16 + 16 * t + r);
+        soff[t] = __umul24((uint32_t)(row < whave ? row : whave - 1), (uint32_t)a.w_pitch) + (uint32_t)a.D / 2 + (uint32_t)(F32 ? g >> 1 : g);
+    }
+    uint32_t scale[NT], next_scale[NT];
+    mx_f4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = mx_f4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int PARTS = XL + WL;
+    auto fetch_scales = [&](int st) {
+        const int at = (st < stages ? st : stages - 1) * WC;
+        const bool in = at + (F32 ? g >> 1 : g) < nb;             // a block past the row: a scale that is a number
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t b = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(wrows, (int)soff[t], at, 0);
+            next_scale[t] = in ? b : 127u;
+        }
+    };
+    auto fetch_part = [&](int part, int st, char *xl, char *wl) {
+        if (part < XL) {
+            const uint32_t at = xchunk < (a.D - st * STAGE) / (F32 ? 4 : 8) ? xoff[part] : BEYOND;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xrows, (EMB_LDS void *)(xl + (part * THREADS + (tid & ~63)) * 16), 16, (int)at, st * 256, 0, 0);
+        } else {
+            const int u = part - XL;
+            const uint32_t at = wchunk(u) < nb - st * WC ? woff[u] : BEYOND;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wrows, (EMB_LDS void *)(wl + (u * THREADS + (tid & ~63)) * 16), 16, (int)at, st * WC * 16, 0, 0);
+        }
+    };
+    const int xplace = (wm * MT * 16 + r) * 256, wplace = wn * NT * 16 + r;
+    const int wkey = F32 ? (wplace >> 3) & 1 : wide_key_w(wplace), xkey = wide_key_x(r);
+    auto compute = [&](const char *xl, const char *wl, int next, char *xnext, char *wnext) {
+        // W's codes of the whole stage: 16 (8) bytes a row
+        uint32_t code[NT][STEPS];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (F32) {
+                const uint2 v = *reinterpret_cast<const uint2 *>(wl + (wplace + 16 * t) * 32 + (((g >> 1) ^ wkey) * 16) + (g & 1) * 8);
+                code[t][0] = v.x;
+                code[t][1] = v.y;
+            } else {
+                const mx_u4 v = *reinterpret_cast<const mx_u4 *>(wl + (wplace + 16 * t) * 64 + ((g ^ wkey) * 16));
+#pragma unroll
+                for (int k = 0; k < STEPS; ++k) code[t][k] = v[k];
+            }
+            scale[t] = next_scale[t];
+        }
+        // x's registers run one step ahead of the products
+        mx_b8 xb[2][MT][KPARTS];
+        uint4 raw[F32 ? MT : 1][2];
+        auto read_x = [&](int k) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if constexpr (F32) {
+                    raw[i][0] = *reinterpret_cast<const uint4 *>(xl + xplace + i * 4096 + (((4 * g + 2 * k) ^ xkey) * 16));
+                    raw[i][1] = *reinterpret_cast<const uint4 *>(xl + xplace + i * 4096 + (((4 * g + 2 * k + 1) ^ xkey) * 16));
+                } else {
+                    xb[k & 1][i][0] = *reinterpret_cast<const mx_b8 *>(xl + xplace + i * 4096 + (((4 * g + k) ^ xkey) * 16));
+                }
+            }
+        };
+        auto split_x = [&](int k) {
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    mx_b8 p[3];
+                    split_bf16(raw[i][0], raw[i][1], p);
+#pragma unroll
+                    for (int j = 0; j < KPARTS; ++j) xb[k & 1][i][j] = p[j];
+                }
+            }
+        };
+        read_x(0);
+        split_x(0);
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            if (k + 1 < STEPS) read_x(k + 1);
+            if (k == 0) fetch_scales(next);
+#pragma unroll
+            for (int q = k * PARTS / STEPS; q < (k + 1) * PARTS / STEPS; ++q) fetch_part(q, next, xnext, wnext);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const mx_b8 wb = codes_to_bf16(code[t][k], __uint_as_float(scale[t] << 23));
+#pragma unroll
+                for (int j = KPARTS - 1; j >= 0; --j)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+                        acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[k & 1][i][j], acc[i][t], 0, 0, 0);
+            }
+            if (k + 1 < STEPS) split_x(k + 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto ready = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();
+    };
+    auto fetch = [&](int st, char *xl, char *wl) {
+        fetch_scales(st);
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) fetch_part(q, st, xl, wl);
+    };
+    int st = 0;
+    if (stages & 1) {
+        fetch(0, x1, w1);
+        ready();
+        compute(x1, w1, 1, x0, w0);
+        st = 1;
+    } else {
+        fetch(0, x0, w0);
+    }
+    for (; st < stages; st += 2) {
+        ready();
+        compute(x0, w0, st + 1, x1, w1);
+        ready();
+        compute(x1, w1, st + 2, x0, w0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);               // nothing is on its way to LDS when the workgroup ends
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + wm * MT * 16 + 16 * i + r;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < NT / NG; ++j) {
+            const mx_f4(&v)[NG] = reinterpret_cast<const mx_f4(&)[NG]>(acc[i][NG * j]);
+            store_run<NG, OUT_BF16>(a.out, m * a.out_stride, n0 + wn * NT * 16 + 16 * NG * j + 4 * NG * g, a.N, v);
+        }
+    }
+}
+
+template <int XT, bool OUT_BF16>
+int launch_widened(ProductArgs a, hipStream_t s)
+{
+    const int64_t blocks = share_tiles(a, 128, 128);
+    if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((product_widened_kernel<XT, OUT_BF16>), dim3((unsigned)blocks), dim3(256), 0, s, a);
     return EMB_OK;
 }
 
@@ -499,13 +745,14 @@ int dispatch_product(const ProductArgs &a, hipStream_t s)
         if (few) return launch_direct<XT, 1, 2, 8, OUT_BF16>(a, s);
         return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
     }
-    if (a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
+    if (a.M <= 32 || a.x_pitch > MOST_PITCH) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
     if constexpr (XT == X_MXFP4) {
         if (a.D <= 128) return launch_tiled<2, 2, 4, true, OUT_BF16>(a, s);
         if ((a.M + 255) / 256 * ((a.N + 255) / 256) >= 256) return launch_tiled<2, 4, 8, false, OUT_BF16>(a, s);
         return launch_tiled<2, 2, 4, false, OUT_BF16>(a, s);
+    } else {
+        return launch_widened<XT, OUT_BF16>(a, s);
     }
-    return launch_direct<XT, 4, 4, 1, OUT_BF16>(a, s);
 }
 
 }  // namespace
@@ -530,7 +777,7 @@ extern "C" int emb_rows_product(const void *x_dev, int32_t x_dtype, int64_t x_st
     if (!emb_aligned(x_dev, 16) || !emb_aligned(w_rows_dev, 16) || !emb_aligned(out_dev, emb_elem_size(out_dtype))) return EMB_ERR_INVALID_ARG;
     if (M > (int64_t)0x7FFFFFFF || N > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
     const ProductArgs a{static_cast<const char *>(x_dev), static_cast<const char *>(w_rows_dev), x_pitch, row, M, N, D,
-                        static_cast<char *>(out_dev), out_stride, 0, 0};
+                        static_cast<char *>(out_dev), out_stride, 0, 0, 1};
     hipStream_t s = emb_stream(stream);
     const bool b = out_dtype == EMB_BF16;
     int e;

@@ -403,6 +403,36 @@ def test_product(M, N, D, kind, out):
 
 
 @pytest.mark.parametrize("kind", ["mxfp4", "bf16", "f32"])
+@pytest.mark.parametrize("M,N,D", [(4100, 4203, 288), (4500, 4096, 544), (300, 66_000, 160), (8193, 2100, 96)])
+def test_product_of_many_tiles(M, N, D, kind):
+    # enough tiles of the largest kind, an odd and an even number of stages, edges both ways
+    rng = np.random.default_rng(M + N)
+    w = mx.random_rows(rng, N, D, 118, 129)
+    x, xv = _operand(rng, M, D, kind)
+    o = torch.full((M, N), float("nan"), dtype=torch.float32, device=H.DEV)
+    emb.emb_rows_product(x, H.dev(w), D, o)
+    got, wv = o.cpu().numpy(), mx.values(w, D)
+    for rows in (np.arange(0, M, 97), np.arange(M - 140, M)):
+        _check_product(got[rows].astype(np.float64), xv[rows], wv, kind, "f32")
+    cols = np.concatenate((np.arange(0, N, 101), np.arange(N - 70, N)))
+    _check_product(got[:, cols].astype(np.float64), xv, wv[cols], kind, "f32")
+    assert not np.isnan(got).any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_product_of_rows_very_far_apart(kind):
+    M, N, D, stride = 40, 70, 64, 3 << 20          # more than 4 MB from row to row
+    rng = np.random.default_rng(8)
+    x, xv = _operand(rng, M, D, kind)
+    far = torch.full((M, stride), float("nan"), dtype=x.dtype, device=H.DEV)
+    far[:, :D] = x
+    w = mx.random_rows(rng, N, D, 118, 129)
+    o = torch.empty((M, N), dtype=torch.float32, device=H.DEV)
+    emb.emb_rows_product(far[:, :D], H.dev(w), D, o)
+    _check_product(o.cpu().double().numpy(), xv, mx.values(w, D), kind, "f32")
+
+
+@pytest.mark.parametrize("kind", ["mxfp4", "bf16", "f32"])
 @pytest.mark.parametrize("M,N,D", [(3, 40, 96), (70, 150, 288), (300, 280, 64)])
 def test_product_passes_on_nan_and_infinity(M, N, D, kind):
     rng = np.random.default_rng(M + D)
