@@ -557,11 +557,12 @@ __device__ __forceinline__ int w_row_at(int place)
     return (place & ~63) | ((place & 12) << 2) | ((place & 48) >> 2) | (place & 3);
 }
 
-template <int XT, bool OUT_BF16>
+// HALF: tiles of 64 x 128, for few rows of x.
+template <int XT, bool HALF, bool OUT_BF16>
 __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
 {
     constexpr bool F32 = XT == X_F32;
-    constexpr int STAGE = F32 ? 64 : 128, WM = F32 ? 4 : 1, WN = F32 ? 1 : 4, MT = F32 ? 2 : 8, NT = F32 ? 8 : 2, NG = F32 ? 4 : 2;
+    constexpr int STAGE = F32 ? 64 : 128, WM = F32 ? 4 : 1, WN = F32 ? 1 : 4, MT = (F32 ? 2 : 8) / (HALF ? 2 : 1), NT = F32 ? 8 : 2, NG = F32 ? 4 : 2;
     constexpr int BM = WM * MT * 16, BN = WN * NT * 16, THREADS = 256;
     constexpr int XC = 16, WC = STAGE / 32;                       // 16-byte chunks of a row in a stage
     constexpr int XL = BM * XC / THREADS, WL = BN * WC / THREADS; // that a thread fetches
@@ -727,31 +728,185 @@ __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
     }
 }
 
-template <int XT, bool OUT_BF16>
+template <int XT, bool HALF, bool OUT_BF16>
 int launch_widened(ProductArgs a, hipStream_t s)
 {
-    const int64_t blocks = share_tiles(a, 128, 128);
+    const int64_t blocks = share_tiles(a, HALF ? 64 : 128, 128);
     if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((product_widened_kernel<XT, OUT_BF16>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((product_widened_kernel<XT, HALF, OUT_BF16>), dim3((unsigned)blocks), dim3(256), 0, s, a);
     return EMB_OK;
 }
 
+// ---------------------------------------------------------------------------
+// few rows of x in bf16 or fp32
+// ---------------------------------------------------------------------------
+// W passes through registers once, 32 rows a wavefront, and bounds it all; x stands in LDS, in bf16 parts, widened once by
+// the workgroup, as much of K at a time as LDS_X holds (all of it for a single row of up to 8192 fp32 elements).  Rows of x
+// lie a multiple of 256 bytes apart, 16-byte chunk c of row m at c ^ wide_key_x(m) within its 16.
+constexpr int LDS_X = 49152;
+
+template <int XT, int MT, bool OUT_BF16>
+__global__ __launch_bounds__(256) void product_skinny_kernel(ProductArgs a, int rows, int kc)
+{
+    constexpr int NT = 2, KPARTS = XT == X_F32 ? 3 : 1, THREADS = 256;
+    constexpr bool AHEAD = MT == 1;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+    const uint32_t tile = emb_xcd_block(blockIdx.x, gridDim.x);
+    if (tile >= (uint32_t)a.tiles_n * (uint32_t)a.tiles_m) return;   // uniform
+    const uint32_t tn = uniform(tile / (uint32_t)a.tiles_m), tm = tile - tn * (uint32_t)a.tiles_m;
+    const int64_t n0 = ((int64_t)tn * 4 + wave) * (16 * NT), m0 = (int64_t)tm * MT * 16;
+    const int nb = a.D / 32, have = a.M - m0 < rows ? (int)(a.M - m0) : rows;
+    const int part = rows * kc * 2;                       // bytes of one part of x in LDS
+
+    const char *wp[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {                        // (rows in the order that gives a lane 4 * NT neighbouring n)
+        const int64_t n = n0 + 4 * NT * (r >> 2) + 4 * t + (r & 3);
+        wp[t] = a.w + (n < a.N ? n : a.N - 1) * a.w_pitch;
+    }
+    int xrow[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xrow[i] = 16 * i + r < have ? 16 * i + r : have - 1;
+    mx_f4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = mx_f4{0.f, 0.f, 0.f, 0.f};
+
+    // 512 elements of W's rows; with AHEAD requested while the 512 before them are multiplied (1 x 128000 x 2048 bf16 25.6 us,
+    // without 29.8; 32 rows of x 52, without 43.8: too few wavefronts fit)
+    uint4 next_wc[NT][4], next_ws[NT];
+    auto load_w = [&](int b0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            next_ws[t] = load_chunk(wp[t] + a.D / 2 + b0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int b = b0 + 4 * j + g;
+                next_wc[t][j] = make_uint4(0, 0, 0, 0);
+                if (b < nb) next_wc[t][j] = load_chunk(wp[t] + b * 16);
+            }
+        }
+    };
+    if (AHEAD) load_w(0);
+    for (int k0 = 0; k0 < a.D; k0 += kc) {                // uniform
+        if (k0) __syncthreads();                          // everyone is done with the part of K before
+        const int chunks = kc / 8;
+        for (int idx = tid; idx < have * chunks; idx += THREADS) {
+            const int m = idx / chunks, c = idx - m * chunks, k = k0 + c * 8;
+            char *to = lds + m * kc * 2 + ((c & ~15) | ((c ^ wide_key_x(m)) & 15)) * 16;
+            const char *from = a.x + (m0 + m) * a.x_pitch + (int64_t)k * (XT == X_F32 ? 4 : 2);
+            uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;   // past the row's end: zeros
+            if (k < a.D) {
+                lo = load_chunk(from);
+                if (XT == X_F32) hi = load_chunk(from + 16);
+            }
+            if constexpr (XT == X_F32) {
+                mx_b8 p[3];
+                split_bf16(lo, hi, p);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) *reinterpret_cast<mx_b8 *>(to + j * part) = p[j];
+            } else {
+                *reinterpret_cast<uint4 *>(to) = lo;
+            }
+        }
+        __syncthreads();
+        const int end = a.D - k0 < kc ? a.D - k0 : kc;
+        for (int s = 0; s * 512 < end; ++s) {
+            const int b0 = k0 / 32 + s * 16;              // first of 16 blocks
+            if (!AHEAD) load_w(b0);
+            uint4 wc[NT][4], ws[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                ws[t] = next_ws[t];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) wc[t][j] = next_wc[t][j];
+            }
+            if (AHEAD && b0 + 16 < nb) load_w(b0 + 16);   // uniform
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (b0 + 4 * j >= nb) break;              // uniform
+                const bool in = b0 + 4 * j + g < nb;      // blocks past the row: codes 0, a scale that is a number
+                float scale[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) scale[t] = __uint_as_float(in ? ((word_of(ws[t], j) >> (8 * g)) & 255u) << 23 : 127u << 23);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    mx_b8 xb[MT][KPARTS];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int k = 0; k < KPARTS; ++k)
+                            xb[i][k] = *reinterpret_cast<const mx_b8 *>(lds + k * part + xrow[i] * kc * 2 + s * 1024 + j * 256 +
+                                                                       (((4 * g + q) ^ wide_key_x(xrow[i])) & 15) * 16);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const mx_b8 wb = codes_to_bf16(word_of(wc[t][j], q), scale[t]);
+#pragma unroll
+                        for (int k = KPARTS - 1; k >= 0; --k)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[i][k], acc[i][t], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + 16 * i + r;
+        if (m < a.M) store_run<NT, OUT_BF16>(a.out, m * a.out_stride, n0 + 4 * NT * g, a.N, acc[i]);
+    }
+}
+
+template <int XT, int MT, bool OUT_BF16>
+int launch_skinny(ProductArgs a, hipStream_t s)
+{
+    constexpr int PARTS = XT == X_F32 ? 3 : 1;
+    const int rows = a.M < MT * 16 ? (int)a.M : MT * 16;
+    int kc = LDS_X / (rows * 2 * PARTS) / 512 * 512;      // (at least 512)
+    const int all = (a.D + 511) / 512 * 512;
+    if (kc > all) kc = all;
+    a.tiles_m = (a.M + MT * 16 - 1) / (MT * 16);
+    a.tiles_n = (a.N + 127) / 128;
+    if (a.tiles_n > (int64_t)0x7FFFFF00 / a.tiles_m) return EMB_ERR_UNSUPPORTED;
+    const int64_t blocks = emb_round_up_xcds(a.tiles_m * a.tiles_n);
+    hipLaunchKernelGGL((product_skinny_kernel<XT, MT, OUT_BF16>), dim3((unsigned)blocks), dim3(256), (size_t)rows * kc * 2 * PARTS, s, a,
+                       rows, kc);
+    return EMB_OK;
+}
+
+// Which kernel.  Times in us on an MI355X, outputs fp32 unless said.
+//   Few tiles of W's rows (their wavefronts would not fill the chip) and a long K: the wavefronts of a workgroup split K, 16 ways
+//   where there are very few (1 x 4096 x 4096 bf16 5.1, without 9.3; 8 x 512 x 16384 fp32 28, with 8 ways 39).
+//   Few rows of x: W streams through registers; MXFP4 and short rows straight from global memory (16 x 100003 x 64 fp32 7.1,
+//   through LDS 8.5; 32 rows 12 and 19; 64 x 128000 x 2048 MXFP4 44, tiles 50), others with x in LDS (16 x 128000 x 2048 bf16
+//   37, straight 50).  A row of x costs an fp32 product three MFMA, and the tiles for it are the less efficient: three
+//   passes over W are still quicker than one over half-empty tiles (48 x 128000 x 2048: 150 and 188).
+//   Rows of x so far apart that 128 of them pass 32-bit offsets: LDS as well, any number of rows.
 template <int XT, bool OUT_BF16>
 int dispatch_product(const ProductArgs &a, hipStream_t s)
 {
-    // With few tiles the chip is not filled: the wavefronts of a workgroup then split a tile's K.
-    const bool few = (a.M + 15) / 16 * ((a.N + 31) / 32) < 2048 && a.D > 512;
-    if (a.M <= 16 || few) {
-        if (few) return launch_direct<XT, 1, 2, 8, OUT_BF16>(a, s);
-        return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
-    }
-    if (a.M <= 32 || a.x_pitch > MOST_PITCH) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
+    const int64_t tiles = (a.M + 15) / 16 * ((a.N + 31) / 32);
+    if (tiles < 2048 && a.D > 512) return tiles < 256 ? launch_direct<XT, 1, 1, 16, OUT_BF16>(a, s) : launch_direct<XT, 1, 2, 8, OUT_BF16>(a, s);
     if constexpr (XT == X_MXFP4) {
+        if (a.M <= 16) return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
+        if (a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
+        if (a.M <= 64) return launch_direct<XT, 4, 2, 1, OUT_BF16>(a, s);
         if (a.D <= 128) return launch_tiled<2, 2, 4, true, OUT_BF16>(a, s);
         if ((a.M + 255) / 256 * ((a.N + 255) / 256) >= 256) return launch_tiled<2, 4, 8, false, OUT_BF16>(a, s);
         return launch_tiled<2, 2, 4, false, OUT_BF16>(a, s);
     } else {
-        return launch_widened<XT, OUT_BF16>(a, s);
+        constexpr bool BF16 = XT == X_BF16;
+        const bool far = a.x_pitch > MOST_PITCH;
+        if (a.D <= 512 && a.M <= 16) return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
+        if (a.D <= 512 && a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
+        if (a.M <= 16 || (!BF16 && (a.M <= 48 || far))) return launch_skinny<XT, 1, OUT_BF16>(a, s);
+        if constexpr (BF16) {
+            if (a.M <= 32 || far) return launch_skinny<XT, 2, OUT_BF16>(a, s);
+        }
+        if (a.M <= 64) return launch_widened<XT, true, OUT_BF16>(a, s);
+        return launch_widened<XT, false, OUT_BF16>(a, s);
     }
 }
 
