@@ -7,12 +7,10 @@
 // The cache's index and the order of its rows are those of the plain cache
 // (cache_index.h); quant_rows.hip writes the rows.
 //
-// The lookup has the loop of gather_quant.h: a group of LPR = D/16 lanes owns a bag,
-// 16 elements a lane.  The lane that resolves an entry marks the address of a table
-// row (bit 0; rows are 16-byte aligned), and where a row is added, the lanes of
-// a group go one way or the other: 8 or 16 bytes of codes and the scale, or 64
-// (fp32) or 32 (bf16) bytes of the row.  Rows are added in the order of
-// the bag's lookups, whichever side they come from.
+// The lookup has the loop of gather_quant.h: a group of LPR lanes owns a bag, 8 or 16
+// elements a lane.  The lane that resolves an entry marks the address of a table
+// row (bit 0; rows are 16-byte aligned).  Rows are added in the order of the bag's
+// lookups, whichever side they come from.
 #include "cache_index.h"
 #include "emb_internal.h"
 #include "gather_quant.h"
@@ -32,88 +30,121 @@ struct QuantCachedSource {
     uint32_t hits, misses;
     bool hashed;
     uint64_t salt, magic;
-    __device__ __forceinline__ uint64_t resolve(int64_t r, int64_t)
+    // An entry is resolved in two steps, so that the index can be asked for a batch ahead: its table row (num_rows for
+    // one that is skipped) and entry of the index, then the address.
+    __device__ __forceinline__ uint64_t row_of(int64_t r) const
     {
         if (hashed) r = (int64_t)emb_fast_mod(emb_splitmix64((uint64_t)r ^ salt), num_rows, magic);
-        if ((uint64_t)r >= num_rows) {
-            emb_flag(status, EMB_STATUS_BAD_INDEX);
-            return 0ull;
-        }
-        const int64_t slot = cache_probe(index, (uint64_t)r, num_hot);
+        if ((uint64_t)r < num_rows) return (uint64_t)r;
+        emb_flag(status, EMB_STATUS_BAD_INDEX);
+        return num_rows;
+    }
+    __device__ __forceinline__ uint4 entry_of(uint64_t r) const   // (for a skipped one any entry)
+    {
+        return load_chunk(reinterpret_cast<const char *>(index + ((r < num_rows ? r : 0) >> 6)));
+    }
+    __device__ __forceinline__ uint64_t address(uint64_t r, const uint4 &entry)
+    {
+        if (r >= num_rows) return reinterpret_cast<uint64_t>(emb_zero_row);
+        const int64_t slot = cache_slot(entry, (int)(r & 63), num_hot);
         if (slot >= 0) {
             ++hits;
             return reinterpret_cast<uint64_t>(cache_rows + slot * cache_row_bytes);
         }
         ++misses;
-        return reinterpret_cast<uint64_t>(table + r * table_row_bytes) | TABLE_ROW;
+        return reinterpret_cast<uint64_t>(table + (int64_t)r * table_row_bytes) | TABLE_ROW;
     }
 };
 
-// N entries of a group's batch, from entry k0 on, each a cache row or a table row.
-template <int LPR, int FMT, bool BF16, int N, int IPL>
-__device__ __forceinline__ void gather_either_rows(float (&acc)[Q_ELEMS], const uint64_t (&mine)[IPL], int k0, QuantPlace at,
+// The elements of a lane: 8 (rows of up to 512), so that many rows can be in flight, or 16.  Its codes are W words; where they
+// are in a row, and the scale of their block (MXFP4), lanes past the row reading its first ones.
+template <int FMT, int E>
+struct LaneCodes {
+    static constexpr int W = E * (FMT == EMB_FMT_INT8 ? 8 : 4) / 32;
+    static __device__ __forceinline__ QuantPlace place(int l, int32_t D)
+    {
+        const uint32_t at = l * E < D ? (uint32_t)l : 0u;
+        if (FMT == EMB_FMT_MXFP4) return QuantPlace{at * (W * 4), (uint32_t)D / 2u + at * E / 32u};
+        return QuantPlace{8u + at * (W * 4), 0u};
+    }
+    static __device__ __forceinline__ void load(const char *p, uint32_t (&w)[W])
+    {
+        if constexpr (W == 1) {
+            w[0] = *(const EMB_GLOBAL uint32_t *)p;
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 2) {   // (8-byte aligned, as lanes and headers are)
+                const uint2 v = load_u2(p + 4 * i);
+                w[i] = v.x;
+                w[i + 1] = v.y;
+            }
+        }
+    }
+    // hdr: scale byte, or scale and bias
+    static __device__ __forceinline__ void add(const uint32_t (&w)[W], const uint2 &hdr, float (&acc)[E])
+    {
+        const float scale = __uint_as_float(FMT == EMB_FMT_MXFP4 ? hdr.x << 23 : hdr.x), bias = __uint_as_float(hdr.y);
+#pragma unroll
+        for (int h = 0; h < W; ++h) {
+            if constexpr (FMT == EMB_FMT_MXFP4) {
+                const emb_f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[h], scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[h], scale, 1);
+                const emb_f2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[h], scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[h], scale, 3);
+                const float f[8] = {a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[8 * h + i] += f[i];
+            } else if constexpr (FMT == EMB_FMT_INT4) {
+                const uint32_t even = w[h] & 0x0F0F0F0Fu, odd = (w[h] >> 4) & 0x0F0F0F0Fu;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[8 * h + 2 * i] += __builtin_fmaf(scale, (float)((even >> (8 * i)) & 0xFFu), bias);
+                    acc[8 * h + 2 * i + 1] += __builtin_fmaf(scale, (float)((odd >> (8 * i)) & 0xFFu), bias);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[4 * h + i] += __builtin_fmaf(scale, (float)((w[h] >> (8 * i)) & 0xFFu), bias);
+            }
+        }
+    }
+};
+
+// N entries of a group's batch, from entry k0 on, each a cache row or a table row.  Both are read and added, the one that the
+// entry does not select being the row of zeros (which stays in the L1): reads under a branch would share
+// registers and wait for each other, row by row (16 384 bags of 30, one fifth of them misses, 16 elements a lane: 33 us, so 25).
+template <int LPR, int FMT, int E, bool BF16, int N, int IPL>
+__device__ __forceinline__ void gather_either_rows(float (&acc)[E], const uint64_t (&mine)[IPL], int k0, QuantPlace at,
                                                    uint32_t table_off)
 {
-    constexpr int CW = FMT == EMB_FMT_INT8 ? 4 : 2;
-    constexpr int CHUNKS = BF16 ? 2 : 4;      // 16-byte pieces of 16 elements
-    uint4 v[N][CHUNKS];                       // a cache row: codes in the first, scale (and bias) in the second
-    bool from_table[N];
+    typedef LaneCodes<FMT, E> Codes;
+    constexpr int CHUNKS = E * (BF16 ? 2 : 4) / 16;   // 16-byte pieces of a table row
+    uint4 full[N][CHUNKS];
+    uint32_t w[N][Codes::W];
+    uint2 hdr[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const uint64_t p = reinterpret_cast<uint64_t>(group_bcast_ptr<LPR>(mine[IPL == 1 ? 0 : (k0 + i) / LPR], (k0 + i) % LPR));
-        from_table[i] = (p & TABLE_ROW) != 0;
-        const char *row = reinterpret_cast<const char *>(p & ~TABLE_ROW);
-        if (from_table[i]) {
+        const bool from_table = (p & TABLE_ROW) != 0;
+        const char *zeros = reinterpret_cast<const char *>(emb_zero_row), *row = reinterpret_cast<const char *>(p & ~TABLE_ROW);
+        const char *const t = from_table ? row : zeros, *const q = from_table ? zeros : row;
+        Codes::load(q + at.code, w[i]);
+        hdr[i] = FMT == EMB_FMT_MXFP4 ? make_uint2(*(const EMB_GLOBAL uint8_t *)(q + at.scale), 0u) : load_u2(q);
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) v[i][c] = load_chunk(row + table_off + 16 * c);
-        } else if (FMT == EMB_FMT_MXFP4) {
-            const uint2 w = load_u2(row + at.code);
-            v[i][0] = make_uint4(w.x, w.y, 0u, 0u);
-            v[i][1].x = *(const EMB_GLOBAL uint8_t *)(row + at.scale);
-        } else {
-            const uint2 h = load_u2(row), w = load_u2(row + at.code);
-            v[i][1].x = h.x;
-            v[i][1].y = h.y;
-            v[i][0] = make_uint4(w.x, w.y, 0u, 0u);
-            if (FMT == EMB_FMT_INT8) {
-                const uint2 w2 = load_u2(row + at.code + 8);
-                v[i][0].z = w2.x;
-                v[i][0].w = w2.y;
-            }
-        }
+        for (int k = 0; k < CHUNKS; ++k) full[i][k] = load_chunk(t + table_off + 16 * k);
     }
     __builtin_amdgcn_sched_barrier(0);   // every load of the batch before its first add
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (from_table[i]) {
+        Codes::add(w[i], hdr[i], acc);
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                const uint32_t w[4] = {v[i][c].x, v[i][c].y, v[i][c].z, v[i][c].w};
+        for (int k = 0; k < CHUNKS; ++k) {
+            const uint32_t v[4] = {full[i][k].x, full[i][k].y, full[i][k].z, full[i][k].w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (BF16) {
-                        acc[(8 * c + 2 * j) % Q_ELEMS] += __uint_as_float(w[j] << 16);
-                        acc[(8 * c + 2 * j + 1) % Q_ELEMS] += __uint_as_float(w[j] & 0xFFFF0000u);
-                    } else {
-                        acc[4 * c + j] += __uint_as_float(w[j]);
-                    }
+            for (int j = 0; j < 4; ++j) {
+                if (BF16) {
+                    acc[(8 * k + 2 * j) % E] += __uint_as_float(v[j] << 16);
+                    acc[(8 * k + 2 * j + 1) % E] += __uint_as_float(v[j] & 0xFFFF0000u);
+                } else {
+                    acc[(4 * k + j) % E] += __uint_as_float(v[j]);
                 }
-            }
-        } else {
-            const uint32_t all[4] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w};
-            uint32_t w[CW];
-#pragma unroll
-            for (int j = 0; j < CW; ++j) w[j] = all[j];
-            float f[Q_ELEMS];
-            if constexpr (FMT == EMB_FMT_MXFP4) {
-                mx_codes_to_float(w, v[i][1].x, f);
-#pragma unroll
-                for (int x = 0; x < Q_ELEMS; ++x) acc[x] += f[x];
-            } else {
-                const float scale = __uint_as_float(v[i][1].x), bias = __uint_as_float(v[i][1].y);
-                codes_to_float<FMT>(w, f);
-#pragma unroll
-                for (int x = 0; x < Q_ELEMS; ++x) acc[x] += __builtin_fmaf(scale, f[x], bias);
             }
         }
     }
@@ -130,9 +161,9 @@ struct QuantCachedArgs {
     hipStream_t s;
 };
 
-constexpr int QC_UNROLL = 4;   // 16 registers an fp32 row and lane
-
-template <int LPR, int FMT, bool BF16>
+// What bounds the lookup is the time that a batch takes to come (its index entries, then its rows), so batches are long, 128
+// registers of fp32 rows, and the next one's entries are under way with this one's rows.
+template <int LPR, int FMT, int E, bool BF16>
 __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_either_kernel(QuantCachedSource src, int64_t B, int64_t nnz,
                                                                             const int64_t *__restrict__ ids,
                                                                             const int64_t *__restrict__ offsets, int32_t D,
@@ -140,14 +171,15 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_either_kernel(Quan
                                                                             unsigned long long *hit_miss, uint32_t *status)
 {
     constexpr int GROUPS = Q_BLOCK / LPR;
-    constexpr int IPL = QC_UNROLL > LPR ? QC_UNROLL / LPR : 1;
+    constexpr int UNROLL = 128 / E;
+    constexpr int IPL = UNROLL > LPR ? UNROLL / LPR : 1;
     constexpr int IB = IPL * LPR;
     const int l = threadIdx.x % LPR;
     const int64_t bag = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LPR;
     const bool live = bag < B;
-    const bool mine_elems = l * Q_ELEMS < D;
-    const QuantPlace at = quant_place<FMT>(l, D);
-    const uint32_t table_off = mine_elems ? (uint32_t)l * Q_ELEMS * (BF16 ? 2u : 4u) : 0u;
+    const bool mine_elems = l * E < D;
+    const QuantPlace at = LaneCodes<FMT, E>::place(l, D);
+    const uint32_t table_off = mine_elems ? (uint32_t)l * E * (BF16 ? 2u : 4u) : 0u;
     int64_t s = 0, e = 0;
     if (live) {
         s = offsets[bag];
@@ -157,32 +189,45 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_either_kernel(Quan
             s = e = 0;
         }
     }
-    float acc[Q_ELEMS];
+    float acc[E];
 #pragma unroll
-    for (int i = 0; i < Q_ELEMS; ++i) acc[i] = 0.f;
-    const uint64_t zero_row = reinterpret_cast<uint64_t>(emb_zero_row);
-    int64_t next[IPL];
-#pragma unroll
-    for (int m = 0; m < IPL; ++m) {
-        const int64_t j = s + m * LPR + l;
-        next[m] = j < e ? ids[j] : 0;
-    }
-    for (int64_t base = s; base < e; base += IB) {
-        uint64_t mine[IPL];
+    for (int i = 0; i < E; ++i) acc[i] = 0.f;
+    int64_t id[IPL];          // of the batch after the next
+    uint64_t row[IPL];        // of the next batch, with its index entries
+    uint4 entry[IPL];
+    auto fetch_ids = [&](int64_t base) {
 #pragma unroll
         for (int m = 0; m < IPL; ++m) {
             const int64_t j = base + m * LPR + l;
-            mine[m] = 0ull;
-            if (j < e) mine[m] = src.resolve(next[m], j);
-            if (mine[m] == 0ull) mine[m] = zero_row;
-            if (j + IB < e) next[m] = ids[j + IB];
+            if (j < e) id[m] = ids[j];
         }
-#pragma unroll(LPR <= 16 ? IB / QC_UNROLL : 1)
-        for (int u = 0; u < IB / QC_UNROLL; ++u) {
-            const int64_t left = e - base - u * QC_UNROLL;
+    };
+    auto probe = [&](int64_t base) {
+#pragma unroll
+        for (int m = 0; m < IPL; ++m) {
+            const int64_t j = base + m * LPR + l;
+            row[m] = src.num_rows;
+            if (j < e) {
+                row[m] = src.row_of(id[m]);
+                entry[m] = src.entry_of(row[m]);
+            }
+        }
+    };
+    fetch_ids(s);
+    probe(s);
+    fetch_ids(s + IB);
+    for (int64_t base = s; base < e; base += IB) {
+        uint64_t mine[IPL];
+#pragma unroll
+        for (int m = 0; m < IPL; ++m) mine[m] = src.address(row[m], entry[m]);
+        probe(base + IB);
+        fetch_ids(base + 2 * IB);
+#pragma unroll(LPR <= 16 ? IB / UNROLL : 1)
+        for (int u = 0; u < IB / UNROLL; ++u) {
+            const int64_t left = e - base - u * UNROLL;
             if (left > 0)
-                gather_batch<QC_UNROLL>(left, [&](auto n) {
-                    gather_either_rows<LPR, FMT, BF16, decltype(n)::value>(acc, mine, u * QC_UNROLL, at, table_off);
+                gather_batch<UNROLL>(left, [&](auto n) {
+                    gather_either_rows<LPR, FMT, E, BF16, decltype(n)::value>(acc, mine, u * UNROLL, at, table_off);
                 });
         }
     }
@@ -190,9 +235,9 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_either_kernel(Quan
         const int64_t len = e - s;
         const bool mean = (mode == EMB_POOL_MEAN) && len > 0;
         const float flen = (float)len;
-        float4 *o = reinterpret_cast<float4 *>(out + bag * (int64_t)D + l * Q_ELEMS);
+        float4 *o = reinterpret_cast<float4 *>(out + bag * (int64_t)D + l * E);
 #pragma unroll
-        for (int i = 0; i < Q_ELEMS / 4; ++i) {
+        for (int i = 0; i < E / 4; ++i) {
             float4 v = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
             if (mean) v = make_float4(v.x / flen, v.y / flen, v.z / flen, v.w / flen);
             o[i] = v;
@@ -204,19 +249,17 @@ __global__ __launch_bounds__(Q_BLOCK) void bag_forward_cached_either_kernel(Quan
 template <int FMT, bool BF16>
 void launch_cached_either(const QuantCachedArgs &a)
 {
-#define EMB_CE(L)                                                                                                        \
-    hipLaunchKernelGGL((bag_forward_cached_either_kernel<L, FMT, BF16>),                                                 \
+#define EMB_CE(L, E)                                                                                                     \
+    hipLaunchKernelGGL((bag_forward_cached_either_kernel<L, FMT, E, BF16>),                                              \
                        dim3((unsigned)((a.B + Q_BLOCK / L - 1) / (Q_BLOCK / L))), dim3(Q_BLOCK), 0, a.s, a.src, a.B,      \
                        a.nnz, a.ids, a.offsets, a.D, a.mode, a.out, a.hit_miss, a.status)
-    switch (emb_quant_lanes(a.D)) {
-        case 1: EMB_CE(1); break;
-        case 2: EMB_CE(2); break;
-        case 4: EMB_CE(4); break;
-        case 8: EMB_CE(8); break;
-        case 16: EMB_CE(16); break;
-        case 32: EMB_CE(32); break;
-        default: EMB_CE(64);
-    }
+    if (a.D <= 16) EMB_CE(2, 8);
+    else if (a.D <= 32) EMB_CE(4, 8);
+    else if (a.D <= 64) EMB_CE(8, 8);
+    else if (a.D <= 128) EMB_CE(16, 8);
+    else if (a.D <= 256) EMB_CE(32, 8);
+    else if (a.D <= 512) EMB_CE(64, 8);
+    else EMB_CE(64, 16);
 #undef EMB_CE
 }
 
