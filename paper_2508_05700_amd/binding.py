@@ -329,6 +329,14 @@ _TENSORS = {
     "emb_cache_observe_hashed": {2: ("raw", _U64), 4: ("freq", _U32), 5: ("status", _i32)},
     "emb_cache_refresh": {0: ("freq", _U32), 4: ("workspace", _u8), 10: ("old_cache_index", _u8), 12: ("hot_rows_out", _i64),
                           14: ("cache_index", _u8), 15: ("moved", _U64), 16: ("info_out", _U64), 17: ("status", _i32)},
+    "emb_bag_forward": {5: ("rows", _i64), 6: ("offsets", _i64), 10: ("out", _f32), 11: ("status", _i32)},
+    "emb_quantize_rows_from": {},                # (a matrix may have rows apart, a destination may be an address)
+    "emb_dequantize_rows": {0: ("src", _u8)},
+    "emb_rows_product": {4: ("w", _u8)},
+    "emb_cache_rebuild_quantized": {5: ("old_cache_rows", _u8), 6: ("old_cache_index", _u8), 8: ("hot_rows", _i64),
+                                    10: ("cache_rows", _u8), 11: ("cache_index", _u8), 12: ("moved", _U64), 13: ("status", _i32)},
+    "emb_bag_forward_cached_quantized": {5: ("cache_rows", _u8), 6: ("cache_index", _u8), 8: ("rows", _i64), 9: ("offsets", _i64),
+                                         13: ("out", _f32), 14: ("hit_miss", _U64), 15: ("status", _i32)},
 }
 _calls_module = None     # False: there is none
 _entries = {}
@@ -463,11 +471,9 @@ def emb_bag_forward(tables: TableSet, rows: torch.Tensor, offsets: torch.Tensor,
     """``streaming``: the EMB_ROWS_STREAMING hint (rows of this batch are unlikely to be reused)."""
     if offsets.numel() != tables.T * B + 1 or out.numel() != tables.T * B * tables.D:
         raise TypeError("shape mismatch")
-    _check("emb_bag_forward", lib().emb_bag_forward(
-        tables.host_ptr, tables.dev_ptr, tables.T, tables.D, DTYPE[tables.dtype],
-        _ptr(rows, torch.int64, "rows"), _ptr(offsets, torch.int64, "offsets"), int(B), rows.numel(),
-        POOL[mode] | (ROWS_STREAMING if streaming else 0),
-        _ptr(out, torch.float32, "out"), _ptr(status, torch.int32, "status"), _stream()))
+    _check("emb_bag_forward", _entry("emb_bag_forward")(
+        tables.host_ptr, tables.dev_ptr, tables.T, tables.D, DTYPE[tables.dtype], rows, offsets, int(B), rows.numel(),
+        POOL[mode] | (ROWS_STREAMING if streaming else 0), out, status, _stream()))
 
 
 def emb_bag_forward_hashed(tables: TableSet, raw: torch.Tensor, offsets: torch.Tensor, B: int, mode: str,
@@ -593,20 +599,20 @@ def emb_quantize_rows(src: torch.Tensor, dtype: str, dst) -> None:
                                                         _stream()))
 
 
-_PLAIN = {torch.float32: "f32", torch.bfloat16: "bf16"}
+_PLAIN = {torch.float32: DTYPE["f32"], torch.bfloat16: DTYPE["bf16"]}
 
 
 def _rows_2d(t: torch.Tensor, name: str):
     """Pointer, storage type, rows, columns and row stride of a device matrix of fp32 or bf16 whose rows are contiguous."""
-    if t.dtype not in _PLAIN or t.dim() != 2:
+    dtype = _PLAIN.get(t.dtype)
+    if dtype is None or t.dim() != 2:
         raise TypeError(f"{name} must be a matrix of float32 or bfloat16")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    R, D = int(t.shape[0]), int(t.shape[1])
-    if D > 1 and t.stride(1) != 1:
+    (R, D), (stride, step) = t.shape, t.stride()
+    if D > 1 and step != 1:
         raise TypeError(f"{name} must have contiguous rows")
-    stride = int(t.stride(0)) if R > 1 else D   # (of a single row the stride says nothing)
-    return t.data_ptr(), DTYPE[_PLAIN[t.dtype]], R, D, stride
+    return t.data_ptr(), dtype, R, D, stride if R > 1 else D   # (of a single row the stride says nothing)
 
 
 def emb_quantize_rows_from(src: torch.Tensor, dtype: str, dst) -> None:
@@ -619,7 +625,7 @@ def emb_quantize_rows_from(src: torch.Tensor, dtype: str, dst) -> None:
         if dst.numel() != R * emb_row_bytes(D, dtype):
             raise TypeError("dst must hold R * emb_row_bytes bytes")
         dptr = _ptr(dst, torch.uint8, "dst")
-    _check("emb_quantize_rows_from", lib().emb_quantize_rows_from(ptr, sd, stride, R, D, DTYPE[dtype], dptr, _stream()))
+    _check("emb_quantize_rows_from", _entry("emb_quantize_rows_from")(ptr, sd, stride, R, D, DTYPE[dtype], dptr, _stream()))
 
 
 def emb_dequantize_rows(src: torch.Tensor, dtype: str, dst: torch.Tensor) -> None:
@@ -628,8 +634,7 @@ def emb_dequantize_rows(src: torch.Tensor, dtype: str, dst: torch.Tensor) -> Non
     ptr, dd, R, D, stride = _rows_2d(dst, "dst")
     if src.numel() != R * emb_row_bytes(D, dtype):
         raise TypeError("src must hold R * emb_row_bytes bytes")
-    _check("emb_dequantize_rows", lib().emb_dequantize_rows(_ptr(src, torch.uint8, "src"), DTYPE[dtype], R, D, ptr, dd, stride,
-                                                            _stream()))
+    _check("emb_dequantize_rows", _entry("emb_dequantize_rows")(src, DTYPE[dtype], R, D, ptr, dd, stride, _stream()))
 
 
 def emb_rows_product(x: torch.Tensor, w: torch.Tensor, D: int, out: torch.Tensor) -> None:
@@ -646,8 +651,7 @@ def emb_rows_product(x: torch.Tensor, w: torch.Tensor, D: int, out: torch.Tensor
         xptr, xd, xstride = _ptr(x, torch.uint8, "x"), DTYPE["mxfp4"], 0
     else:
         xptr, xd, _, _, xstride = _rows_2d(x, "x")
-    _check("emb_rows_product", lib().emb_rows_product(xptr, xd, xstride, M, _ptr(w, torch.uint8, "w"), N, int(D), optr, od, ostride,
-                                                      _stream()))
+    _check("emb_rows_product", _entry("emb_rows_product")(xptr, xd, xstride, M, w, N, int(D), optr, od, ostride, _stream()))
 
 
 def emb_bag_backward_workspace_bytes(T: int, B: int, nnz: int, total_rows: int, D: int, dtype: str) -> int:
@@ -901,31 +905,20 @@ def emb_cache_rebuild_quantized(table_ptr: int, num_rows: int, D: int, dtype: st
                                 moved: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     if cache_rows.numel() < hot_rows.numel() * emb_row_bytes(D, cache_dtype):
         raise TypeError("cache_rows too small")
-    _check("emb_cache_rebuild_quantized", lib().emb_cache_rebuild_quantized(
-        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype],
-        _ptr(old_cache_rows, torch.uint8, "old_cache_rows"), _ptr(old_cache_index, torch.uint8, "old_cache_index"),
-        int(old_num_hot), _ptr(hot_rows, torch.int64, "hot_rows"), hot_rows.numel(),
-        _ptr(cache_rows, torch.uint8, "cache_rows"), _ptr(cache_index, torch.uint8, "cache_index"), _ptr(moved, _U64, "moved"),
-        _ptr(status, torch.int32, "status"), _stream()))
-
-
-def _forward_cached_quantized(fn: str, table_ptr, num_rows, D, dtype, cache_dtype, cache_rows, cache_index, num_hot, salt, ids,
-                              id_dtype, offsets, B, mode, out, hit_miss, status):
-    if offsets.numel() != B + 1 or out.numel() != B * D:
-        raise TypeError("shape mismatch")
-    _check(fn, getattr(lib(), fn)(
-        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], _ptr(cache_rows, torch.uint8, "cache_rows"),
-        _ptr(cache_index, torch.uint8, "cache_index"), int(num_hot), *salt, _ptr(ids, id_dtype, "ids"),
-        _ptr(offsets, torch.int64, "offsets"), int(B), ids.numel(), POOL[mode], _ptr(out, torch.float32, "out"),
-        _ptr(hit_miss, _U64, "hit_miss"), _ptr(status, torch.int32, "status"), _stream()))
+    _check("emb_cache_rebuild_quantized", _entry("emb_cache_rebuild_quantized")(
+        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], old_cache_rows, old_cache_index,
+        int(old_num_hot), hot_rows, hot_rows.numel(), cache_rows, cache_index, moved, status, _stream()))
 
 
 def emb_bag_forward_cached_quantized(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str,
                                      cache_rows: torch.Tensor, cache_index: torch.Tensor, num_hot: int, rows: torch.Tensor,
                                      offsets: torch.Tensor, B: int, mode: str, out: torch.Tensor,
                                      hit_miss: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
-    _forward_cached_quantized("emb_bag_forward_cached_quantized", table_ptr, num_rows, D, dtype, cache_dtype, cache_rows,
-                              cache_index, num_hot, (), rows, torch.int64, offsets, B, mode, out, hit_miss, status)
+    if offsets.numel() != B + 1 or out.numel() != B * D:
+        raise TypeError("shape mismatch")
+    _check("emb_bag_forward_cached_quantized", _entry("emb_bag_forward_cached_quantized")(
+        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], cache_rows, cache_index, int(num_hot), rows,
+        offsets, int(B), rows.numel(), POOL[mode], out, hit_miss, status, _stream()))
 
 
 def emb_bag_forward_cached_quantized_hashed(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str,
@@ -933,9 +926,13 @@ def emb_bag_forward_cached_quantized_hashed(table_ptr: int, num_rows: int, D: in
                                             raw: torch.Tensor, offsets: torch.Tensor, B: int, mode: str, out: torch.Tensor,
                                             hit_miss: Optional[torch.Tensor] = None,
                                             status: Optional[torch.Tensor] = None) -> None:
-    _forward_cached_quantized("emb_bag_forward_cached_quantized_hashed", table_ptr, num_rows, D, dtype, cache_dtype, cache_rows,
-                              cache_index, num_hot, (C.c_uint64(int(salt) % (1 << 64)),), raw, _U64, offsets, B, mode, out,
-                              hit_miss, status)
+    if offsets.numel() != B + 1 or out.numel() != B * D:
+        raise TypeError("shape mismatch")
+    _check("emb_bag_forward_cached_quantized_hashed", lib().emb_bag_forward_cached_quantized_hashed(
+        int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], _ptr(cache_rows, torch.uint8, "cache_rows"),
+        _ptr(cache_index, torch.uint8, "cache_index"), int(num_hot), C.c_uint64(int(salt) % (1 << 64)), _ptr(raw, _U64, "raw"),
+        _ptr(offsets, torch.int64, "offsets"), int(B), raw.numel(), POOL[mode], _ptr(out, torch.float32, "out"),
+        _ptr(hit_miss, _U64, "hit_miss"), _ptr(status, torch.int32, "status"), _stream()))
 
 
 def emb_bag_forward_cached(table_ptr: int, num_rows: int, D: int, dtype: str, cache_rows: torch.Tensor,

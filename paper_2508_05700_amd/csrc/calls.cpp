@@ -131,6 +131,12 @@ Entry entries[] = {
     EMB_ENTRY(emb_bag_forward_cached_tables_hashed_lengths),
     EMB_ENTRY(emb_cache_observe_hashed),
     EMB_ENTRY(emb_cache_refresh),
+    EMB_ENTRY(emb_bag_forward),
+    EMB_ENTRY(emb_quantize_rows_from),
+    EMB_ENTRY(emb_dequantize_rows),
+    EMB_ENTRY(emb_rows_product),
+    EMB_ENTRY(emb_cache_rebuild_quantized),
+    EMB_ENTRY(emb_bag_forward_cached_quantized),
 };
 constexpr long N_ENTRIES = sizeof(entries) / sizeof(entries[0]);
 
