@@ -21,7 +21,6 @@ typedef int mx_i8 __attribute__((ext_vector_type(8)));
 typedef float mx_f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 mx_b8 __attribute__((ext_vector_type(8)));
 typedef float mx_f4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef __bf16 mx_b4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef __bf16 mx_b8_any __attribute__((ext_vector_type(8), aligned(2)));
 
 enum { X_MXFP4 = 0, X_BF16 = 1, X_F32 = 2 };
@@ -43,6 +42,18 @@ __device__ __forceinline__ mx_i8 mx_operand(const uint4 &v)
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int j) { return j == 0 ? v.x : (j == 1 ? v.y : (j == 2 ? v.z : v.w)); }
+
+// The unit's tiles take W's rows in an order that makes a lane's results 16 neighbouring bytes of the output and those of
+// its four lane groups 64: for fp32 the rows' own, for bf16 place 16 * (2 * j + t) + 4 * a + b is row 32 * j + 4 * (2 * a + t) + b, so
+// that two tiles end as 8 neighbouring n.  (Pieces of 16 bytes that only the L2 joins cost more the larger the output:
+// 512 x 400000 x 128 to fp32 270 us, so 189.)
+template <bool OUT_BF16>
+constexpr int TILES = OUT_BF16 ? 2 : 1;   // that a store takes together
+template <bool OUT_BF16>
+__device__ __forceinline__ int w_row_at(int place)
+{
+    return OUT_BF16 ? (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3) : place;
+}
 
 // 4 * V neighbouring elements of a row of the output, v[0] the first four.
 template <int V, bool OUT_BF16>
@@ -76,6 +87,18 @@ __device__ __forceinline__ void store_run(char *out, int64_t row, int64_t n, int
             }
         }
     }
+}
+
+// A lane's results for row m of x: NT tiles whose first place is n0.
+template <int NT, bool OUT_BF16>
+__device__ __forceinline__ void store_tiles(const ProductArgs &a, int64_t m, int64_t n0, int g, const mx_f4 (&v)[NT])
+{
+    constexpr int V = TILES<OUT_BF16>;
+    static_assert(NT % V == 0, "whole stores");
+    if (m >= a.M) return;
+#pragma unroll
+    for (int j = 0; j < NT / V; ++j)
+        store_run<V, OUT_BF16>(a.out, m * a.out_stride, n0 + 16 * V * j + 4 * V * g, a.N, reinterpret_cast<const mx_f4(&)[V]>(v[V * j]));
 }
 
 // 8 codes of one word, by their block's power of two, as bf16 (exact)
@@ -124,7 +147,7 @@ __global__ __launch_bounds__(KS > 1 ? 64 * KS : 256) void product_direct_kernel(
     const char *wp[NT], *xp[MT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {                    // rows past the end: the last row, not stored
-        const int64_t n = n0 + 16 * t + r;
+        const int64_t n = n0 + (NT % TILES<OUT_BF16> == 0 ? w_row_at<OUT_BF16>(16 * t + r) : 16 * t + r);
         wp[t] = a.w + (n < a.N ? n : a.N - 1) * a.w_pitch;
     }
 #pragma unroll
@@ -235,29 +258,13 @@ __global__ __launch_bounds__(KS > 1 ? 64 * KS : 256) void product_direct_kernel(
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + 16 * i + r;
-        if (m >= a.M) continue;
+        if constexpr (NT % TILES<OUT_BF16> == 0) {
+            store_tiles<NT, OUT_BF16>(a, m0 + 16 * i + r, n0, g, acc[i]);
+        } else if (m0 + 16 * i + r < a.M) {               // a single tile to bf16
+            __bf16 *o = reinterpret_cast<__bf16 *>(a.out) + (m0 + 16 * i + r) * a.out_stride + n0 + 4 * g;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int64_t n = n0 + 16 * t + 4 * g;
-            if constexpr (OUT_BF16) {
-                __bf16 *o = reinterpret_cast<__bf16 *>(a.out) + m * a.out_stride + n;
-                const mx_b4_any v = {(__bf16)acc[i][t][0], (__bf16)acc[i][t][1], (__bf16)acc[i][t][2], (__bf16)acc[i][t][3]};
-                if (n + 4 <= a.N) {
-                    *reinterpret_cast<mx_b4_any *>(o) = v;
-                } else {
-                    for (int k = 0; k < 4; ++k)
-                        if (n + k < a.N) o[k] = (__bf16)acc[i][t][k];
-                }
-            } else {
-                float *o = reinterpret_cast<float *>(a.out) + m * a.out_stride + n;
-                if (n + 4 <= a.N) {
-                    *reinterpret_cast<mx_f4_any *>(o) = acc[i][t];
-                } else {
-                    for (int k = 0; k < 4; ++k)
-                        if (n + k < a.N) o[k] = acc[i][t][k];
-                }
-            }
+            for (int k = 0; k < 4; ++k)
+                if (n0 + 4 * g + k < a.N) o[k] = (__bf16)acc[i][0][k];
         }
     }
 }
@@ -288,10 +295,8 @@ typedef uint32_t mx_u4 __attribute__((ext_vector_type(4)));
 // 256 elements of a row are 8 chunks of 16 bytes; a tile keeps them in 128 bytes a row, chunk c at place c ^ key(row).  LDS
 // serves a 16-byte read 16 lanes at a time, of which 8 are of one lane group (rows 0-3 and 12-15 of a tile, or 4-11) and 8 of
 // its neighbour (the other rows): groups that read neighbouring chunks then find 16 different places of 256 bytes.
-// W's tiles of the matrix unit take rows 16 * (i / 4) + 4 * t + i % 4 (i: the unit's row, t: tile), so that a lane's four
-// tiles end as 16 neighbouring n; x's take 16 neighbouring rows.
-__device__ __forceinline__ int key_x(int row) { return (row >> 1) & 7; }
-__device__ __forceinline__ int key_w(int row) { return ((row >> 1) & 1) | ((row >> 3) & 6); }
+// W's rows stand there in the order of the unit's tiles (w_row_at).
+__device__ __forceinline__ int key_of(int place) { return (place >> 1) & 7; }
 
 constexpr int STAGE_CHUNKS = 8;
 
@@ -319,15 +324,14 @@ __device__ __forceinline__ bool tile_of(const ProductArgs &a, uint32_t &tm, uint
 constexpr uint32_t BUFFER_END = 1u << 30, BEYOND = 1u << 31;
 constexpr int64_t MOST_PITCH = 1 << 22;    // of rows of x that are tiled: 128 of them end below BUFFER_END, as 256 MXFP4 rows do (34816 bytes)
 
-template <int ROWS, int THREADS, bool IS_W>
+template <int ROWS, int THREADS, bool IS_W, bool OUT_BF16>
 struct StageOperand {
     static constexpr int LOADS = ROWS * STAGE_CHUNKS / THREADS;
     __amdgpu_buffer_rsrc_t rows;
-    uint32_t off[LOADS];       // of this thread's chunk of row u * THREADS / 8 + threadIdx / 8
+    uint32_t off[LOADS];       // of this thread's chunk of the row at place u * THREADS / 8 + threadIdx / 8
     __device__ __forceinline__ static int chunk(int u)
     {
-        const int row = u * (THREADS / STAGE_CHUNKS) + threadIdx.x / STAGE_CHUNKS;
-        return (threadIdx.x % STAGE_CHUNKS) ^ (IS_W ? key_w(row) : key_x(row));
+        return (threadIdx.x % STAGE_CHUNKS) ^ key_of(u * (THREADS / STAGE_CHUNKS) + threadIdx.x / STAGE_CHUNKS);
     }
     // have: how many rows there are (the others repeat the last)
     __device__ __forceinline__ void init(const char *base, int64_t have, int64_t pitch)
@@ -335,7 +339,7 @@ struct StageOperand {
         rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, BUFFER_END, 0x00020000);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int row = u * (THREADS / STAGE_CHUNKS) + threadIdx.x / STAGE_CHUNKS;
+            const int place = u * (THREADS / STAGE_CHUNKS) + threadIdx.x / STAGE_CHUNKS, row = IS_W ? w_row_at<OUT_BF16>(place) : place;
             off[u] = __umul24((uint32_t)(row < have ? row : (int)have - 1), (uint32_t)pitch) + 16u * (uint32_t)chunk(u);
         }
     }
@@ -365,20 +369,19 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
     const int64_t xrows = a.M - m0, wrows = a.N - n0;
     const int nb = a.D / 32, stages = (nb + STAGE_CHUNKS - 1) / STAGE_CHUNKS, last = nb - (stages - 1) * STAGE_CHUNKS;
 
-    StageOperand<BM, THREADS, false> xo;
-    StageOperand<BN, THREADS, true> wo;
+    StageOperand<BM, THREADS, false, OUT_BF16> xo;
+    StageOperand<BN, THREADS, true, OUT_BF16> wo;
     xo.init(xbase, xrows < BM ? xrows : BM, a.x_pitch);
     wo.init(wbase, wrows < BN ? wrows : BN, a.w_pitch);
     const char *srow;                                 // the scales that this thread fetches
     {
         const int64_t have = tid < BM ? xrows : wrows;
-        int64_t row = tid < BM ? tid : tid - BM;
+        int64_t row = tid < BM ? tid : w_row_at<OUT_BF16>(tid - BM);
         if (row >= have) row = have - 1;
         srow = (tid < BM ? xbase + row * a.x_pitch : wbase + row * a.w_pitch) + a.D / 2;
     }
-    // the lane's first row in either tile; its others lie 16 rows (x) and 4 rows (W) on, with the same key
-    const int xrow0 = wm * MT * 16 + r, wrow0 = wn * 64 + 16 * (r >> 2) + (r & 3);
-    const int xkey = key_x(xrow0), wkey = key_w(wrow0);
+    // the lane's first place in either tile; its others lie 16 places on, with the same key
+    const int xrow0 = wm * MT * 16 + r, wrow0 = wn * 64 + r, key = key_of(r);
     uint2 sc;
     mx_f4 acc[MT][NT];
 #pragma unroll
@@ -403,9 +406,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
     // first tile, then in the second.  One read gives a lane the scales of two tiles and both steps.
     int splace;
     {
-        const int row = tid < BM ? tid : tid - BM;
-        const int in_tile = tid < BM ? row & 15 : ((row >> 2) & 12) | (row & 3), t = tid < BM ? row >> 4 : (row >> 6) * 4 + ((row >> 2) & 3);
-        splace = (tid < BM ? 0 : BM * 4) + ((t >> 1) * 16 + in_tile) * 8 + (t & 1);
+        const int place = tid < BM ? tid : tid - BM;
+        splace = (tid < BM ? 0 : BM * 4) + ((place >> 5) * 16 + (place & 15)) * 8 + ((place >> 4) & 1);
     }
     auto ready = [&](int st, uint16_t *sl) {
         __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this thread's chunks of the stage are in LDS
@@ -439,12 +441,12 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
         auto read_w = [&](int step) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                wv[step][t] = *reinterpret_cast<const mx_u4 *>(wl + wrow0 * 128 + (((4 * step + g) ^ wkey) * 16) + t * 512);
+                wv[step][t] = *reinterpret_cast<const mx_u4 *>(wl + wrow0 * 128 + (((4 * step + g) ^ key) * 16) + t * 2048);
         };
         auto read_x = [&](int q) {
 #pragma unroll
             for (int i = 0; i < XG; ++i)
-                xv[q & 1][i] = *reinterpret_cast<const mx_u4 *>(xl + xrow0 * 128 + (((4 * (q / PER_STEP) + g) ^ xkey) * 16) +
+                xv[q & 1][i] = *reinterpret_cast<const mx_u4 *>(xl + xrow0 * 128 + (((4 * (q / PER_STEP) + g) ^ key) * 16) +
                                                                 ((q % PER_STEP) * XG + i) * 2048);
         };
         read_w(0);
@@ -507,9 +509,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(ProductArgs
 
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + wm * MT * 16 + 16 * i + r, n = n0 + wn * 64 + 16 * g;
-        if (m >= a.M) continue;
-        store_run<NT, OUT_BF16>(a.out, m * a.out_stride, n, a.N, acc[i]);
+        store_tiles<NT, OUT_BF16>(a, m0 + wm * MT * 16 + 16 * i + r, n0 + wn * 64, g, acc[i]);
     }
 }
 
@@ -545,24 +545,15 @@ int launch_tiled(ProductArgs a, hipStream_t s)
 // takes the stage's elements from g * STAGE / 4 on, in steps of 8: chunk c of a row of x stands at place c ^ wide_key_x(row).
 // Tiles are 128 x 128.  bf16: by wavefronts of 128 x 32, so that W's codes are widened once; two workgroups fill a CU's LDS
 // exactly.  fp32: by wavefronts of 32 x 128, so that every element of x is split into its three parts once.
-// W's rows stand in LDS in the order in which the unit's tiles take them: place 16 * (N * j + t) + 4 * a + b holds row
-// 16 * N * j + 4 * (N * a + t) + b, so that a lane's N tiles end as 4 * N neighbouring n (N = 2 or 4).
 // Keys for rows of 256 bytes, chunks 4 apart in neighbouring lane groups, and of 64 bytes, chunks 1 apart.
 __device__ __forceinline__ int wide_key_x(int row) { return (row & 3) | ((row >> 1) & 4) | (((row << 1) ^ row) & 8); }
 __device__ __forceinline__ int wide_key_w(int row) { return ((row >> 1) & 2) ^ ((row >> 3) & 1) * 3; }
-template <int N>
-__device__ __forceinline__ int w_row_at(int place)
-{
-    if (N == 2) return (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3);
-    return (place & ~63) | ((place & 12) << 2) | ((place & 48) >> 2) | (place & 3);
-}
-
 // HALF: tiles of 64 x 128, for few rows of x.
 template <int XT, bool HALF, bool OUT_BF16>
 __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
 {
     constexpr bool F32 = XT == X_F32;
-    constexpr int STAGE = F32 ? 64 : 128, WM = F32 ? 4 : 1, WN = F32 ? 1 : 4, MT = (F32 ? 2 : 8) / (HALF ? 2 : 1), NT = F32 ? 8 : 2, NG = F32 ? 4 : 2;
+    constexpr int STAGE = F32 ? 64 : 128, WM = F32 ? 4 : 1, WN = F32 ? 1 : 4, MT = (F32 ? 2 : 8) / (HALF ? 2 : 1), NT = F32 ? 8 : 2;
     constexpr int BM = WM * MT * 16, BN = WN * NT * 16, THREADS = 256;
     constexpr int XC = 16, WC = STAGE / 32;                       // 16-byte chunks of a row in a stage
     constexpr int XL = BM * XC / THREADS, WL = BN * WC / THREADS; // that a thread fetches
@@ -591,12 +582,12 @@ __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
     }
 #pragma unroll
     for (int u = 0; u < WL; ++u) {
-        const int row = w_row_at<NG>((u * THREADS + tid) / WC);
+        const int row = w_row_at<OUT_BF16>((u * THREADS + tid) / WC);
         woff[u] = __umul24((uint32_t)(row < whave ? row : whave - 1), (uint32_t)a.w_pitch) + 16u * (uint32_t)wchunk(u);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int row = w_row_at<NG>(wn * NT * 16 + 16 * t + r);
+        const int row = w_row_at<OUT_BF16>(wn * NT * 16 + 16 * t + r);
         soff[t] = __umul24((uint32_t)(row < whave ? row : whave - 1), (uint32_t)a.w_pitch) + (uint32_t)a.D / 2 + (uint32_t)(F32 ? g >> 1 : g);
     }
     uint32_t scale[NT], next_scale[NT];
@@ -718,13 +709,7 @@ __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
     __builtin_amdgcn_s_waitcnt(0x0F70);               // nothing is on its way to LDS when the workgroup ends
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + wm * MT * 16 + 16 * i + r;
-        if (m >= a.M) continue;
-#pragma unroll
-        for (int j = 0; j < NT / NG; ++j) {
-            const mx_f4(&v)[NG] = reinterpret_cast<const mx_f4(&)[NG]>(acc[i][NG * j]);
-            store_run<NG, OUT_BF16>(a.out, m * a.out_stride, n0 + wn * NT * 16 + 16 * NG * j + 4 * NG * g, a.N, v);
-        }
+        store_tiles<NT, OUT_BF16>(a, m0 + wm * MT * 16 + 16 * i + r, n0 + wn * NT * 16, g, acc[i]);
     }
 }
 
@@ -761,8 +746,8 @@ __global__ __launch_bounds__(256) void product_skinny_kernel(ProductArgs a, int 
 
     const char *wp[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {                        // (rows in the order that gives a lane 4 * NT neighbouring n)
-        const int64_t n = n0 + 4 * NT * (r >> 2) + 4 * t + (r & 3);
+    for (int t = 0; t < NT; ++t) {
+        const int64_t n = n0 + w_row_at<OUT_BF16>(16 * t + r);
         wp[t] = a.w + (n < a.N ? n : a.N - 1) * a.w_pitch;
     }
     int xrow[MT];
@@ -854,8 +839,7 @@ __global__ __launch_bounds__(256) void product_skinny_kernel(ProductArgs a, int 
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + 16 * i + r;
-        if (m < a.M) store_run<NT, OUT_BF16>(a.out, m * a.out_stride, n0 + 4 * NT * g, a.N, acc[i]);
+        store_tiles<NT, OUT_BF16>(a, m0 + 16 * i + r, n0, g, acc[i]);
     }
 }
 
