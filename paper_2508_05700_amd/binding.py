@@ -581,6 +581,7 @@ def emb_bag_forward_mixed(mt: MixedTables, rows: torch.Tensor, offsets: torch.Te
         rows.numel(), POOL[mode], out, out.numel(), status, _stream()))
 
 
+@functools.lru_cache(maxsize=1024)   # (asking the library takes as long as the rest of a call's marshalling)
 def emb_row_bytes(D: int, dtype: str) -> int:
     return int(lib().emb_row_bytes(int(D), DTYPE[dtype]))
 
