@@ -210,6 +210,64 @@ def test_lookups_over_mxfp4_rows(T, B, R, D, max_len, mode):
     assert st.item() == 0
 
 
+def test_versions_refresh_and_bag_lengths_of_hosted_mxfp4_tables():
+    # the remaining lookups that take the type: latched tables, hosted sets from bag lengths, and a policy-run cache of its own type
+    rng = np.random.default_rng(12)
+    T, R, D, B = 2, 300, 96, 37
+    packed = [mx.random_rows(rng, R, D) for _ in range(T)]
+    vals = [mx.values(p, D) for p in packed]
+    dev = [H.dev(p) for p in packed]
+    lengths, off, _ = _batch(rng, T, B, R, 15)
+    raw = rng.integers(0, 1 << 63, size=int(off[-1]), dtype=np.int64)
+    ts = emb.TableSet(dev, D, "mxfp4", salts=[5, 6])
+    st = _status()
+    rows, out = torch.empty(raw.size, dtype=torch.int64, device=H.DEV), torch.empty((T, B, D), device=H.DEV)
+    off_out = torch.empty(T * B + 1, dtype=torch.int64, device=H.DEV)
+    scratch = torch.empty(emb.emb_offsets_scratch_bytes(T * B), dtype=torch.uint8, device=H.DEV)
+    emb.emb_bag_forward_hashed_lengths(ts, H.dev(raw), H.dev(lengths), B, "mean", out, off_out, scratch, rows, st)
+    first = out.cpu().numpy()
+    _check_pool(first, vals, rows.cpu().numpy(), off, B, "mean")
+    handle = torch.zeros(1, dtype=torch.int64, device=H.DEV)
+    record = torch.empty(emb.emb_version_record_bytes(T), dtype=torch.uint8, device=H.DEV)
+    latch = torch.empty(emb.emb_version_latch_bytes(T), dtype=torch.uint8, device=H.DEV)
+    emb.emb_version_record_write(record, ts, 3)
+    emb.emb_version_publish(handle, record)
+    emb.emb_version_latch(handle, T, latch, st)
+    out.fill_(9.0)
+    emb.emb_bag_forward_latched_hashed(latch, T, D, "mxfp4", H.dev(raw), H.dev(off), B, "mean", out, st)
+    assert np.array_equal(out.cpu().numpy(), first)
+    caches = [pipeline.HotRowCache(dev[t].data_ptr(), R, D, "mxfp4", 40, 5 + t, torch.device(H.DEV)) for t in range(T)]
+    hosted = pipeline.HostedTableSet(caches, torch.device(H.DEV))
+    for _ in range(2):
+        out.fill_(9.0)
+        emb.emb_bag_forward_cached_tables_hashed_lengths(hosted.tables, H.dev(raw), H.dev(lengths), B, "mean", out, off_out, scratch,
+                                                         None, st)
+        assert np.array_equal(out.cpu().numpy(), first)
+        hosted.observe(H.dev(raw), off, B)
+        hosted.refresh()
+    assert st.item() == 0 and all(c.status.item() == 0 for c in caches)
+
+
+def test_batches_without_lookups():
+    R, D, B = 50, 64, 3
+    packed = mx.random_rows(np.random.default_rng(1), R, D)
+    none, off = torch.empty(0, dtype=torch.int64, device=H.DEV), torch.zeros(B + 1, dtype=torch.int64, device=H.DEV)
+    out = torch.full((1, B, D), 9.0, device=H.DEV)
+    emb.emb_bag_forward(emb.TableSet([H.dev(packed)], D, "mxfp4"), none, off, B, "mean", out)
+    assert not out.any()
+    t = torch.ones((R, D), device=H.DEV)
+    index = torch.empty(emb.emb_cache_index_bytes(R), dtype=torch.uint8, device=H.DEV)
+    cache = torch.empty((1, 48), dtype=torch.uint8, device=H.DEV)
+    emb.emb_cache_build_quantized(t.data_ptr(), R, D, "f32", "mxfp4", none, cache, index)
+    out.fill_(9.0)
+    emb.emb_bag_forward_cached_quantized(t.data_ptr(), R, D, "f32", "mxfp4", cache, index, 0, none, off, B, "mean", out)
+    assert not out.any()
+    emb.emb_quantize_rows_from(t[:0], "mxfp4", cache[:0])
+    emb.emb_dequantize_rows(cache[:0], "mxfp4", t[:0])
+    emb.emb_rows_product(t[:0], cache, D, torch.empty((0, 1), device=H.DEV))
+    emb.emb_rows_product(t, cache[:0], D, torch.empty((R, 0), device=H.DEV))
+
+
 def test_lookups_skip_bad_rows_and_bags_and_pass_on_nan():
     rng = np.random.default_rng(5)
     R, D, B = 40, 64, 5
