@@ -873,6 +873,7 @@ def emb_bag_backward_rowwise_adagrad(tables: TableSet, rows: torch.Tensor, offse
         _stream()))
 
 
+@functools.lru_cache(maxsize=1024)   # (as emb_row_bytes)
 def emb_cache_index_bytes(num_rows: int) -> int:
     out = C.c_size_t(0)
     _check("emb_cache_index_bytes", lib().emb_cache_index_bytes(int(num_rows), C.byref(out)))
@@ -888,12 +889,20 @@ def emb_cache_build(table_ptr: int, num_rows: int, D: int, dtype: str, hot_rows:
         _ptr(cache_index, torch.uint8, "cache_index"), _ptr(status, torch.int32, "status"), _stream()))
 
 
+def _check_quantized_cache(cache_rows: Optional[torch.Tensor], cache_index: Optional[torch.Tensor], num_hot: int, num_rows: int,
+                           D: int, cache_dtype: str, name: str) -> None:
+    """A cache of ``num_hot`` rows fits its tensors (the kernels trust the numbers)."""
+    if num_hot > 0 and (cache_rows is None or cache_rows.numel() < num_hot * emb_row_bytes(D, cache_dtype)):
+        raise TypeError(name + "_rows too small")
+    if cache_index is not None and cache_index.numel() < emb_cache_index_bytes(num_rows):
+        raise TypeError(name + "_index too small")
+
+
 def emb_cache_build_quantized(table_ptr: int, num_rows: int, D: int, dtype: str, cache_dtype: str, hot_rows: torch.Tensor,
                               cache_rows: torch.Tensor, cache_index: torch.Tensor,
                               status: Optional[torch.Tensor] = None) -> None:
     """``emb_cache_build`` with rows of ``cache_dtype`` (a quantised type), made from the table's as they are written."""
-    if cache_rows.numel() < hot_rows.numel() * emb_row_bytes(D, cache_dtype):
-        raise TypeError("cache_rows too small")
+    _check_quantized_cache(cache_rows, cache_index, hot_rows.numel(), num_rows, D, cache_dtype, "cache")
     _check("emb_cache_build_quantized", lib().emb_cache_build_quantized(
         int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], _ptr(hot_rows, torch.int64, "hot_rows"),
         hot_rows.numel(), _ptr(cache_rows, torch.uint8, "cache_rows"), _ptr(cache_index, torch.uint8, "cache_index"),
@@ -904,8 +913,8 @@ def emb_cache_rebuild_quantized(table_ptr: int, num_rows: int, D: int, dtype: st
                                 old_cache_rows: Optional[torch.Tensor], old_cache_index: torch.Tensor, old_num_hot: int,
                                 hot_rows: torch.Tensor, cache_rows: torch.Tensor, cache_index: torch.Tensor,
                                 moved: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
-    if cache_rows.numel() < hot_rows.numel() * emb_row_bytes(D, cache_dtype):
-        raise TypeError("cache_rows too small")
+    _check_quantized_cache(cache_rows, cache_index, hot_rows.numel(), num_rows, D, cache_dtype, "cache")
+    _check_quantized_cache(old_cache_rows, old_cache_index, old_num_hot, num_rows, D, cache_dtype, "old_cache")
     _check("emb_cache_rebuild_quantized", _entry("emb_cache_rebuild_quantized")(
         int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], old_cache_rows, old_cache_index,
         int(old_num_hot), hot_rows, hot_rows.numel(), cache_rows, cache_index, moved, status, _stream()))
@@ -917,6 +926,7 @@ def emb_bag_forward_cached_quantized(table_ptr: int, num_rows: int, D: int, dtyp
                                      hit_miss: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     if offsets.numel() != B + 1 or out.numel() != B * D:
         raise TypeError("shape mismatch")
+    _check_quantized_cache(cache_rows, cache_index, num_hot, num_rows, D, cache_dtype, "cache")
     _check("emb_bag_forward_cached_quantized", _entry("emb_bag_forward_cached_quantized")(
         int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], cache_rows, cache_index, int(num_hot), rows,
         offsets, int(B), rows.numel(), POOL[mode], out, hit_miss, status, _stream()))
@@ -929,6 +939,7 @@ def emb_bag_forward_cached_quantized_hashed(table_ptr: int, num_rows: int, D: in
                                             status: Optional[torch.Tensor] = None) -> None:
     if offsets.numel() != B + 1 or out.numel() != B * D:
         raise TypeError("shape mismatch")
+    _check_quantized_cache(cache_rows, cache_index, num_hot, num_rows, D, cache_dtype, "cache")
     _check("emb_bag_forward_cached_quantized_hashed", lib().emb_bag_forward_cached_quantized_hashed(
         int(table_ptr), int(num_rows), int(D), DTYPE[dtype], DTYPE[cache_dtype], _ptr(cache_rows, torch.uint8, "cache_rows"),
         _ptr(cache_index, torch.uint8, "cache_index"), int(num_hot), C.c_uint64(int(salt) % (1 << 64)), _ptr(raw, _U64, "raw"),

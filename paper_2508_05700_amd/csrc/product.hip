@@ -269,6 +269,9 @@ __global__ __launch_bounds__(KS > 1 ? 64 * KS : 256) void product_direct_kernel(
     }
 }
 
+// A grid holds fewer than 2^32 threads.
+inline bool fits_a_grid(int64_t blocks, int64_t threads) { return blocks <= (int64_t)0xFFFFFFFF / threads; }
+
 template <int XT, int MT, int NT, int KS, bool OUT_BF16>
 int launch_direct(ProductArgs a, hipStream_t s)
 {
@@ -277,6 +280,7 @@ int launch_direct(ProductArgs a, hipStream_t s)
     a.tiles_n = (a.N + cols - 1) / cols;
     if (a.tiles_n > (int64_t)0x7FFFFF00 / a.tiles_m) return EMB_ERR_UNSUPPORTED;
     const int64_t blocks = emb_round_up_xcds(a.tiles_m * a.tiles_n);
+    if (!fits_a_grid(blocks, KS > 1 ? 64 * KS : 256)) return EMB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((product_direct_kernel<XT, MT, NT, KS, OUT_BF16>), dim3((unsigned)blocks), dim3(KS > 1 ? 64 * KS : 256), 0, s, a);
     return EMB_OK;
 }
@@ -535,7 +539,7 @@ template <int WM, int WN, int MT, bool ONE, bool OUT_BF16>
 int launch_tiled(ProductArgs a, hipStream_t s)
 {
     const int64_t blocks = share_tiles(a, WM * MT * 16, WN * 64);
-    if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
+    if (!fits_a_grid(blocks, 64 * WM * WN)) return EMB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((product_tiled_kernel<WM, WN, MT, ONE, OUT_BF16>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, a);
     return EMB_OK;
 }
@@ -717,7 +721,7 @@ template <int XT, bool HALF, bool OUT_BF16>
 int launch_widened(ProductArgs a, hipStream_t s)
 {
     const int64_t blocks = share_tiles(a, HALF ? 64 : 128, 128);
-    if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
+    if (!fits_a_grid(blocks, 256)) return EMB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((product_widened_kernel<XT, HALF, OUT_BF16>), dim3((unsigned)blocks), dim3(256), 0, s, a);
     return EMB_OK;
 }
@@ -855,6 +859,7 @@ int launch_skinny(ProductArgs a, hipStream_t s)
     a.tiles_n = (a.N + 127) / 128;
     if (a.tiles_n > (int64_t)0x7FFFFF00 / a.tiles_m) return EMB_ERR_UNSUPPORTED;
     const int64_t blocks = emb_round_up_xcds(a.tiles_m * a.tiles_n);
+    if (!fits_a_grid(blocks, 256)) return EMB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((product_skinny_kernel<XT, MT, OUT_BF16>), dim3((unsigned)blocks), dim3(256), (size_t)rows * kc * 2 * PARTS, s, a,
                        rows, kc);
     return EMB_OK;

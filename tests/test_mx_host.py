@@ -1,6 +1,7 @@
 """MXFP4 rows, the product with them and the quantised cache without a GPU: sizes, refusals, and the plain forms."""
 import numpy as np
 import pytest
+import torch
 
 from paper_2508_05700_amd import binding as b
 from tests import mx_plain
@@ -73,6 +74,7 @@ def test_product_refusals(L):
     assert f(*args(out=FAKE + 1, od=BF16)) == INVALID
     assert f(*args(D=48, xs=48)) == UNSUPPORTED and f(*args(D=65568, xs=65568)) == UNSUPPORTED and f(*args(D=0)) == INVALID
     assert f(*args(M=1 << 31)) == UNSUPPORTED and f(*args(N=1 << 31, os=1 << 31)) == UNSUPPORTED
+    assert f(*args(D=32, M=1, N=(1 << 31) - 1, os=1 << 31)) == UNSUPPORTED       # more threads than a grid holds
     assert f(*args(xd=MX, xs=0, M=0)) == OK                                      # the stride of MXFP4 rows is their size
 
 
@@ -103,6 +105,24 @@ def test_quantized_cache_refusals(L):
     hh = L.emb_bag_forward_cached_quantized_hashed
     a = args(ids=None)
     assert hh(*(a[:8] + [7] + a[8:])) == INVALID
+
+
+def test_a_quantized_cache_that_does_not_fit_its_tensors_is_refused():
+    # 100 rows of 64 elements: rows of 48 bytes, an index of 2 entries of 16
+    u8 = lambda n: torch.zeros(n, dtype=torch.uint8)
+    ids, offs, out = torch.zeros(8, dtype=torch.int64), torch.zeros(5, dtype=torch.int64), torch.zeros(4, 64)
+    lookup = lambda rows, index: b.emb_bag_forward_cached_quantized(4096, 100, 64, "f32", "mxfp4", rows, index, 10, ids, offs, 4,
+                                                                      "sum", out)
+    hashed = lambda rows, index: b.emb_bag_forward_cached_quantized_hashed(4096, 100, 64, "f32", "mxfp4", rows, index, 10, 7, ids,
+                                                                             offs, 4, "sum", out)
+    build = lambda rows, index: b.emb_cache_build_quantized(4096, 100, 64, "f32", "mxfp4", ids, rows, index)
+    rebuild = lambda rows, index: b.emb_cache_rebuild_quantized(4096, 100, 64, "f32", "mxfp4", rows, index, 10, ids, u8(480), u8(32))
+    rebuild_to = lambda rows, index: b.emb_cache_rebuild_quantized(4096, 100, 64, "f32", "mxfp4", u8(480), u8(32), 10, ids, rows, index)
+    for call, need in ((lookup, 480), (hashed, 480), (build, 8 * 48), (rebuild, 480), (rebuild_to, 8 * 48)):
+        with pytest.raises(TypeError, match="rows too small"):
+            call(u8(need - 1), u8(32))
+        with pytest.raises(TypeError, match="index too small"):
+            call(u8(need), u8(31))
 
 
 def test_plain_form_of_the_definition():
