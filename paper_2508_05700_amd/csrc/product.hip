@@ -873,6 +873,34 @@ int launch_skinny(ProductArgs a, hipStream_t s)
 //   37, straight 50).  A row of x costs an fp32 product three MFMA, and the tiles for it are the less efficient: three
 //   passes over W are still quicker than one over half-empty tiles (48 x 128000 x 2048: 150 and 188).
 //   Rows of x so far apart that 128 of them pass 32-bit offsets: LDS as well, any number of rows.
+//   Up to 32 rows of x past whole tiles: a call of their own, where their tiles would begin another round of workgroups on the
+//   chip (at_once of them) and rows are long enough for that to take longer than the call (4099 rows of x, 4096 of W: 1024 elements
+//   bf16 45.2, so 42.7, fp32 180, so 163; 4096: MXFP4 63.8, so 44.1, bf16 167, so 142; with 512 elements bf16 nothing is won).
+inline int64_t rows_of_full_rounds(const ProductArgs &a, int64_t tile, int64_t at_once)
+{
+    const int64_t whole = a.M / tile * tile, rest = a.M - whole;
+    if (whole == 0 || rest == 0 || rest > 32) return a.M;
+    ProductArgs all = a, without = a;
+    without.M = whole;
+    return (share_tiles(without, tile, tile) + at_once - 1) / at_once < (share_tiles(all, tile, tile) + at_once - 1) / at_once ? whole : a.M;
+}
+
+template <int XT, bool OUT_BF16>
+int dispatch_product(const ProductArgs &a, hipStream_t s);
+
+template <int XT, bool OUT_BF16>
+int dispatch_in_two(ProductArgs a, int64_t whole, hipStream_t s)
+{
+    const int64_t rest = a.M - whole;
+    a.M = whole;
+    const int rc = dispatch_product<XT, OUT_BF16>(a, s);
+    if (rc != EMB_OK) return rc;
+    a.M = rest;
+    a.x += whole * a.x_pitch;
+    a.out += whole * a.out_stride * (OUT_BF16 ? 2 : 4);
+    return dispatch_product<XT, OUT_BF16>(a, s);
+}
+
 template <int XT, bool OUT_BF16>
 int dispatch_product(const ProductArgs &a, hipStream_t s)
 {
@@ -883,7 +911,12 @@ int dispatch_product(const ProductArgs &a, hipStream_t s)
         if (a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
         if (a.M <= 64) return launch_direct<XT, 4, 2, 1, OUT_BF16>(a, s);
         if (a.D <= 128) return launch_tiled<2, 2, 4, true, OUT_BF16>(a, s);
-        if ((a.M + 255) / 256 * ((a.N + 255) / 256) >= 256) return launch_tiled<2, 4, 8, false, OUT_BF16>(a, s);
+        const bool big = (a.M + 255) / 256 * ((a.N + 255) / 256) >= 256;
+        if (a.D >= 512 && a.N <= 65536) {             // (a strip of more tiles is rounds by itself, and the few rows read all of W)
+            const int64_t whole = rows_of_full_rounds(a, big ? 256 : 128, big ? 256 : 512);
+            if (whole < a.M) return dispatch_in_two<XT, OUT_BF16>(a, whole, s);
+        }
+        if (big) return launch_tiled<2, 4, 8, false, OUT_BF16>(a, s);
         return launch_tiled<2, 2, 4, false, OUT_BF16>(a, s);
     } else {
         constexpr bool BF16 = XT == X_BF16;
@@ -895,6 +928,10 @@ int dispatch_product(const ProductArgs &a, hipStream_t s)
             if (a.M <= 32 || far) return launch_skinny<XT, 2, OUT_BF16>(a, s);
         }
         if (a.M <= 64) return launch_widened<XT, true, OUT_BF16>(a, s);
+        if (a.D >= (BF16 ? 1024 : 512)) {
+            const int64_t whole = rows_of_full_rounds(a, 128, 512);
+            if (whole < a.M) return dispatch_in_two<XT, OUT_BF16>(a, whole, s);
+        }
         return launch_widened<XT, false, OUT_BF16>(a, s);
     }
 }

@@ -477,6 +477,23 @@ def test_product_of_many_tiles(M, N, D, kind):
     assert not np.isnan(got).any()
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["mxfp4", "bf16", "f32"])
+@pytest.mark.parametrize("M,N,D", [(4099, 4096, 1056), (1054, 8190, 1024), (513, 16_300, 1504), (288, 32_768, 1024)])
+def test_product_of_a_few_rows_past_whole_tiles(M, N, D, kind, out):
+    rng = np.random.default_rng(M + N + D)
+    w = mx.random_rows(rng, N, D, 118, 129)
+    x, xv = _operand(rng, M, D, kind, pad=8)
+    o = torch.full((M + 1, N + 5), 3.0, dtype=TORCH[out], device=H.DEV)
+    emb.emb_rows_product(x, H.dev(w), D, o[:M, :N])
+    got, wv = o.cpu().float().numpy(), mx.values(w, D)
+    assert (got[M] == 3.0).all() and (got[:, N:] == 3.0).all()
+    for rows in (np.arange(0, M, 193), np.arange(M - 40, M)):
+        _check_product(got[rows, :N].astype(np.float64), xv[rows], wv, kind, out)
+    cols = np.concatenate((np.arange(0, N, 401), np.arange(N - 20, N)))
+    _check_product(got[:M, cols].astype(np.float64), xv, wv[cols], kind, out)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_product_of_rows_very_far_apart(kind):
     M, N, D, stride = 40, 70, 64, 3 << 20          # more than 4 MB from row to row
