@@ -110,19 +110,17 @@ __device__ __forceinline__ mx_b8 codes_to_bf16(uint32_t w, float scale)
 }
 
 // Eight fp32 values as three bf16 parts: the upper 8 bits of the significand, the 8 after them and the last 8, all cut off, not
-// rounded.  An infinity or a NaN is the first part alone.
+// rounded.  An infinity is the first part alone; of a NaN the other parts are NaN, wherever its mark is.
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 __device__ __forceinline__ void split_bf16(const uint4 &a, const uint4 &b, mx_b8 (&p)[3])
 {
-    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, mid[8], low[8];
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t mid[8], low[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t top = w[i] & 0x7FFFFFFFu;
-        const bool finite = top < 0x7F800000u;
-        const float r = __uint_as_float(w[i]) - __uint_as_float(w[i] & 0xFFFF0000u);
-        mid[i] = finite ? __float_as_uint(r) : 0u;
+        const float f = __uint_as_float(w[i]), r = f - __uint_as_float(w[i] & 0xFFFF0000u);
+        mid[i] = __builtin_fabsf(f) == __builtin_inff() ? 0u : __float_as_uint(r);
         low[i] = __float_as_uint(__uint_as_float(mid[i]) - __uint_as_float(mid[i] & 0xFFFF0000u));
-        if (top > 0x7F800000u) w[i] |= 0x00400000u;   // a NaN whose mark is in the lower half stays one
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
