@@ -863,13 +863,20 @@ int launch_skinny(ProductArgs a, hipStream_t s)
     return EMB_OK;
 }
 
-// Which kernel.  Times in us on an MI355X, outputs fp32 unless said.
-//   Few tiles of W's rows (their wavefronts would not fill the chip) and a long K: the wavefronts of a workgroup split K, 16 ways
-//   where there are very few (1 x 4096 x 4096 bf16 5.1, without 9.3; 8 x 512 x 16384 fp32 28, with 8 ways 39).
-//   Few rows of x: W streams through registers; MXFP4 and short rows straight from global memory (16 x 100003 x 64 fp32 7.1,
-//   through LDS 8.5; 32 rows 12 and 19; 64 x 128000 x 2048 MXFP4 44, tiles 50), others with x in LDS (16 x 128000 x 2048 bf16
-//   37, straight 50).  A row of x costs an fp32 product three MFMA, and the tiles for it are the less efficient: three
-//   passes over W are still quicker than one over half-empty tiles (48 x 128000 x 2048: 150 and 188).
+// Which kernel.  Times in us on an MI355X, outputs bf16 unless said.
+//   A long K and tiles of 16 x 32 too few to fill the chip with wavefronts: the wavefronts of a workgroup split K, 16 ways where there
+//   are very few (1 x 4096 x 4096 bf16 5.1, without 9.3; 8 x 512 x 16384 fp32 25, with 8 ways 39).  Beyond about 1024 tiles the other
+//   kernels fill it (16 x 50000 x 512 bf16 5.3, split 12.9); the split parts of fp32, for which every wavefront makes three parts of its
+//   x, lose from 512 on (1024 x 512 x 1024 8.9, split 18.8); few rows of MXFP4 that are very long, which have no other kernel that shares
+//   a tile, gain up to 2048 (32 x 16384 x 4096 16.5, without 31).
+//   Few rows of x: W streams through registers; MXFP4 and short rows straight from global memory (16 x 100003 x 64 fp32 6.4,
+//   through LDS 8.5; from 256 elements on LDS is ahead: 16 x 100003 x 512 bf16 8.9, straight 11.6, fp32 11.9 and 19.4), others with x in
+//   LDS (16 x 128000 x 2048 bf16 37, straight 50).  33 to 64 rows of MXFP4 are tiles where they are long and W has not rows enough for
+//   straight wavefronts (64 x 16384 x 4096 16.5, straight 31; 64 x 128000 x 2048 44, tiles 50).
+//   A row of x costs an fp32 product three MFMA, and the tiles for it are the less efficient: three passes over W are still quicker
+//   than one over half-empty tiles (48 x 128000 x 2048: 114 and 188), and any number of them where tiles do not fill the
+//   chip once (256 x 4096 x 1024 12.2, tiles 38.6; 512 x 2048 x 4096 46 and 142; the shorter the rows, the sooner tiles are ahead: 256 x 16384 x 256
+//   16.4 and 13.9, 512 x 4096 x 256 9.5 and 12.9).  bf16 takes half tiles there (512 x 4096 x 4096 29, whole 37.6).
 //   Rows of x so far apart that 128 of them pass 32-bit offsets: LDS as well, any number of rows.
 //   Up to 32 rows of x past whole tiles: a call of their own, where their tiles would begin another round of workgroups on the
 //   chip (at_once of them) and rows are long enough for that to take longer than the call (4099 rows of x, 4096 of W: 1024 elements
@@ -903,11 +910,12 @@ template <int XT, bool OUT_BF16>
 int dispatch_product(const ProductArgs &a, hipStream_t s)
 {
     const int64_t tiles = (a.M + 15) / 16 * ((a.N + 31) / 32);
-    if (tiles < 2048 && a.D > 512) return tiles < 256 ? launch_direct<XT, 1, 1, 16, OUT_BF16>(a, s) : launch_direct<XT, 1, 2, 8, OUT_BF16>(a, s);
+    const int64_t most_split = XT == X_F32 ? 512 : (XT == X_MXFP4 && a.M <= 32 && a.D >= 2048 ? 2048 : 1024);
+    if (a.D > 512 && tiles <= most_split) return tiles < 256 ? launch_direct<XT, 1, 1, 16, OUT_BF16>(a, s) : launch_direct<XT, 1, 2, 8, OUT_BF16>(a, s);
     if constexpr (XT == X_MXFP4) {
         if (a.M <= 16) return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
         if (a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
-        if (a.M <= 64) return launch_direct<XT, 4, 2, 1, OUT_BF16>(a, s);
+        if (a.M <= 64 && (a.D < 1024 || a.N >= 65536)) return launch_direct<XT, 4, 2, 1, OUT_BF16>(a, s);
         if (a.D <= 128) return launch_tiled<2, 2, 4, true, OUT_BF16>(a, s);
         const bool big = (a.M + 255) / 256 * ((a.N + 255) / 256) >= 256;
         if (a.D >= 512 && a.N <= 65536) {             // (a strip of more tiles is rounds by itself, and the few rows read all of W)
@@ -919,13 +927,14 @@ int dispatch_product(const ProductArgs &a, hipStream_t s)
     } else {
         constexpr bool BF16 = XT == X_BF16;
         const bool far = a.x_pitch > MOST_PITCH;
-        if (a.D <= 512 && a.M <= 16) return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
-        if (a.D <= 512 && a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
-        if (a.M <= 16 || (!BF16 && (a.M <= 48 || far))) return launch_skinny<XT, 1, OUT_BF16>(a, s);
+        const int64_t strips = (a.N + 127) / 128;
+        if (a.D < 256 && a.M <= 16) return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
+        if (a.D < 256 && a.M <= 32) return launch_direct<XT, 2, 2, 1, OUT_BF16>(a, s);
+        if (a.M <= 16 || (!BF16 && (a.M <= 48 || far || (a.M + 127) / 128 * strips < (a.D >= 512 ? 512 : 160)))) return launch_skinny<XT, 1, OUT_BF16>(a, s);
         if constexpr (BF16) {
             if (a.M <= 32 || far) return launch_skinny<XT, 2, OUT_BF16>(a, s);
         }
-        if (a.M <= 64) return launch_widened<XT, true, OUT_BF16>(a, s);
+        if (a.M <= 64 || (BF16 && (a.M + 63) / 64 * strips <= 512)) return launch_widened<XT, true, OUT_BF16>(a, s);
         if (a.D >= (BF16 ? 1024 : 512)) {
             const int64_t whole = rows_of_full_rounds(a, 128, 512);
             if (whole < a.M) return dispatch_in_two<XT, OUT_BF16>(a, whole, s);

@@ -441,7 +441,7 @@ def _check_product(got, x, w, kind, out):
 
 SHAPES = [(1, 1, 32), (1, 1000, 64), (1, 37, 2048), (2, 17, 96), (15, 64, 128), (16, 257, 160), (17, 16, 512), (31, 100, 544),
           (33, 130, 1056), (64, 63, 32), (65, 4, 64), (100, 513, 64), (129, 255, 320), (257, 300, 4096), (300, 1, 128), (5, 700, 16384),
-          (512, 512, 1024)]
+          (512, 512, 1024), (30, 90, 96), (60, 70_000, 96), (50, 66_000, 1024), (20, 50_001, 256)]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
