@@ -445,7 +445,8 @@ int emb_dequantize_rows(const void *src_dev, int32_t dtype, int64_t num_rows, in
  * nearest-even once); out_stride in elements, >= N; elements between the rows are
  * not written.  A NaN or infinity of x or W reaches the sums it takes part in, as in
  * fp32.  x_dev and w_rows_dev 16-byte aligned; out_dev aligned to its elements; it
- * must not overlap them.  Any M and N from 0 up to 2^31 - 2048.
+ * must not overlap them.  Any M and N from 0 up to 2^31 - 2048.  Like the
+ * lookups of quantised tables it has no backward: the rows are the result of training.
  * EMB_ERR_UNSUPPORTED if D is not a multiple of 32 or above 65536, or M or N is larger. */
 int emb_rows_product(const void *x_dev, int32_t x_dtype, int64_t x_stride, int64_t M,
                      const void *w_rows_dev, int64_t N, int32_t D, void *out_dev,

