@@ -40,19 +40,19 @@ def log(*a):
 # bytes or less are counted at their true size, so for kernels that issue those (4-byte accumulators,
 # 48-byte quantised rows) the scaled figure is an upper bound.
 PMC_TRAFFIC = {
-    "sources": "0b1ec5e7d557a228",
+    "sources": "445dbbf400e8fb86",
     "fetch_scale": 2.0,
     "write_scale": 1.0,
     "kib_per_launch": {     # workload -> kernel -> (FETCH_SIZE, WRITE_SIZE)
-        "3": {"bag_forward_train_kernel": (173340.4, 69738.3), "update_kernel": (240611.1, 324005.1)},
-        "3b": {"bag_forward_train_kernel": (90490.6, 74007.8), "update_kernel": (170068.4, 220938.5)},
-        "2": {"bag_forward_kernel<HASHED>": (172137.4, 33876.3), "bag_forward_kernel": (172188.2, 32768.0)},
-        "2u": {"bag_forward_kernel<HASHED>": (338204.0, 33799.4), "bag_forward_kernel": (338159.2, 32768.0)},
-        "2un": {"bag_forward_kernel": (339613.5, 32768.0)},
-        "2q4": {"bag_forward_quant_kernel": (112553.2, 33832.4)},
-        "2uq4": {"bag_forward_quant_kernel": (224857.4, 33900.7)},
-        "2uq4r": {"bag_forward_quant_kernel": (182296.5, 33863.8)},
-        "4": {"bag_forward_kernel<HASHED>": (52430.9, 8704.2)},
+        "3": {"bag_forward_train_kernel": (173324.8, 69748.9), "update_kernel": (240613.9, 324004.0)},
+        "3b": {"bag_forward_train_kernel": (90494.7, 73991.4), "update_kernel": (170033.2, 220969.5)},
+        "2": {"bag_forward_kernel<HASHED>": (172110.4, 33875.4), "bag_forward_kernel": (172180.1, 32768.0)},
+        "2u": {"bag_forward_kernel<HASHED>": (338205.7, 33799.4), "bag_forward_kernel": (338157.7, 32768.0)},
+        "2un": {"bag_forward_kernel": (339629.8, 32768.0)},
+        "2q4": {"bag_forward_quant_kernel": (112585.3, 33832.8)},
+        "2uq4": {"bag_forward_quant_kernel": (224866.8, 33904.1)},
+        "2uq4r": {"bag_forward_quant_kernel": (182427.6, 33863.3)},
+        "4": {"bag_forward_kernel<HASHED>": (52451.3, 8704.3)},
     },
 }
 
