@@ -444,7 +444,9 @@ int emb_dequantize_rows(const void *src_dev, int32_t dtype, int64_t num_rows, in
  * deterministic.  out_dtype: EMB_F32, or EMB_BF16 (the sum rounded to
  * nearest-even once); out_stride in elements, >= N; elements between the rows are
  * not written.  A NaN or infinity of x or W reaches the sums it takes part in, as in
- * fp32.  x_dev and w_rows_dev 16-byte aligned; out_dev aligned to its elements; it
+ * fp32 (with x in EMB_MXFP4 elements beyond the range of fp32 are numbers like the
+ * others; with x in EMB_F32 sums that an infinite element of W takes part in may be made
+ * in the order of the elements).  x_dev and w_rows_dev 16-byte aligned; out_dev aligned to its elements; it
  * must not overlap them.  Any M and N from 0 up to 2^31 - 2048.  Like the
  * lookups of quantised tables it has no backward: the rows are the result of training.
  * EMB_ERR_UNSUPPORTED if D is not a multiple of 32 or above 65536, or M or N is larger. */

@@ -8,6 +8,7 @@
 // exact, sums are fp32.  With x in bf16, W's elements become bf16, exactly, and the product is
 // bf16's.  With x in fp32, x = h + m + l with three bf16 parts of 8 bits each, exact unless a
 // part falls below bf16's range: three bf16 products with the same W, summed in fp32 from the smallest part on.
+// (Infinite elements of W are for redo_infinite_rows.)
 //
 // A wavefront holds a tile of 16*NT rows of W and 16*MT rows of x.  W is the unit's
 // row operand, so that a lane ends with four neighbouring n of one m: one 16-byte store.
@@ -128,6 +129,55 @@ __device__ __forceinline__ void split_bf16(const uint4 &a, const uint4 &b, mx_b8
         const uint32_t(&from)[8] = k == 0 ? w : (k == 1 ? mid : low);
         p[k] = __builtin_bit_cast(mx_b8, make_uint4(upper_halves(from[0], from[1]), upper_halves(from[2], from[3]),
                                                     upper_halves(from[4], from[5]), upper_halves(from[6], from[7])));
+    }
+}
+
+// Rows of W with infinite elements (under a scale byte of 253 or 254: 4 and 6 by 2^126, 2 to 6 by 2^127; the quantisers here
+// write none) and an fp32 x.  A part of x that is zero makes NaN of an infinity, where fp32 has the infinity that the other parts
+// make of it (theirs have the same sign, so nothing but NaN is ever wrong).  A wavefront with a NaN among its sums therefore
+// looks at such results in its tile again, and makes those of rows with such bytes an element of x at a time.  (Seen at the
+// end of a tile, for nothing: a maximum of the scale bytes kept along the way took 2 to 3 % of 4096 x 4096 x 1024.)
+template <int ROWS, int COLS, bool OUT_BF16>
+__device__ __forceinline__ void redo_infinite_rows(const ProductArgs &a, int64_t m0, int64_t n0)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what the wavefront has stored is in its place
+    for (int at = threadIdx.x & 63; at < ROWS * COLS; at += 64) {
+        const int64_t m = m0 + at / COLS, n = n0 + at % COLS;
+        if (m >= a.M || n >= a.N) continue;
+        float *const o32 = reinterpret_cast<float *>(a.out) + m * a.out_stride + n;
+        __bf16 *const o16 = reinterpret_cast<__bf16 *>(a.out) + m * a.out_stride + n;
+        const float was = OUT_BF16 ? (float)*o16 : *o32;
+        if (was == was) continue;
+        const char *const w = a.w + n * a.w_pitch, *const scales = w + a.D / 2, *const x = a.x + m * a.x_pitch;
+        bool infinite = false;
+        for (int b = 0; b < a.D / 32; ++b) infinite |= *(const EMB_GLOBAL uint8_t *)(scales + b) - 253u < 2u;
+        if (!infinite) continue;
+        float sum = 0.f;
+        for (int c = 0; c < a.D / 4; ++c) {            // 4 elements
+            const uint32_t codes = *(const EMB_GLOBAL uint16_t *)(w + 2 * c), byte = *(const EMB_GLOBAL uint8_t *)(scales + c / 8);
+            const float scale = __uint_as_float(byte << 23);
+            const emb_f2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+            const uint4 v = load_chunk(x + 16 * c);
+            sum = __builtin_fmaf(__uint_as_float(v.x), lo.x, sum);
+            sum = __builtin_fmaf(__uint_as_float(v.y), lo.y, sum);
+            sum = __builtin_fmaf(__uint_as_float(v.z), hi.x, sum);
+            sum = __builtin_fmaf(__uint_as_float(v.w), hi.y, sum);
+        }
+        if (OUT_BF16) *o16 = (__bf16)sum;
+        else *o32 = sum;
+    }
+}
+// acc: the wavefront's sums, stored; every lane calls this.
+template <int XT, bool OUT_BF16, int MT, int NT>
+__device__ __forceinline__ void mend_infinite_rows(const ProductArgs &a, int64_t m0, int64_t n0, const mx_f4 (&acc)[MT][NT])
+{
+    if constexpr (XT == X_F32) {
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < MT * NT; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) nan |= acc[i / NT][i % NT][k] != acc[i / NT][i % NT][k];
+        if (__any(nan)) redo_infinite_rows<16 * MT, 16 * NT, OUT_BF16>(a, m0, n0);
     }
 }
 
@@ -266,6 +316,7 @@ __global__ __launch_bounds__(KS > 1 ? 64 * KS : 256) void product_direct_kernel(
                 if (n0 + 4 * g + k < a.N) o[k] = (__bf16)acc[i][0][k];
         }
     }
+    mend_infinite_rows<XT, OUT_BF16>(a, m0, n0, acc);
 }
 
 // A grid holds fewer than 2^32 threads.
@@ -742,6 +793,7 @@ __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
     for (int i = 0; i < MT; ++i) {
         store_tiles<NT, OUT_BF16>(a, m0 + wm * MT * 16 + 16 * i + r, n0 + wn * NT * 16, g, acc[i]);
     }
+    mend_infinite_rows<XT, OUT_BF16>(a, m0 + wm * MT * 16, n0 + wn * NT * 16, acc);
 }
 
 template <int XT, bool HALF, bool OUT_BF16>
@@ -872,6 +924,7 @@ __global__ __launch_bounds__(256) void product_skinny_kernel(ProductArgs a, int 
     for (int i = 0; i < MT; ++i) {
         store_tiles<NT, OUT_BF16>(a, m0 + 16 * i + r, n0, g, acc[i]);
     }
+    mend_infinite_rows<XT, OUT_BF16>(a, m0, n0, acc);
 }
 
 template <int XT, int MT, bool OUT_BF16>
