@@ -67,3 +67,79 @@ def test_product_with_rows_beyond_the_range_of_fp32(M, N, D, kind, out):
         if out == "bf16":
             tol = tol + 2.0 ** -8 * (np.abs(ref[keep]) + tol)
         assert np.all(np.abs(g[keep, n] - ref[keep]) <= tol), n
+
+
+@pytest.mark.parametrize("M,N,D", PRODUCTS)
+def test_product_of_fp32_keeps_every_bit_in_every_kernel(M, N, D):
+    # one element of 24 bits a row of x, by a power of two: the product is exact, and each of the three parts of x takes part in
+    # it.  Over the passes the element goes over every place of a block, over the blocks and over the rows of a tile.
+    rng = np.random.default_rng(M * 3 + N + D)
+    w = mx.pack(rng.choice(np.array([1, 2, 4, 6, 9, 10, 12, 14], dtype=np.uint8), (N, D)), rng.integers(120, 130, (N, D // 32), dtype=np.uint8))
+    wv = torch.from_numpy(mx.values(w, D)).to(H.DEV)
+    wd = H.dev(w)
+    rows = torch.arange(M, device=H.DEV)
+    got = torch.empty((M, N), device=H.DEV)
+    for k in range(8):
+        at = torch.from_numpy((np.arange(M) * 37 + k * (D // 8 + 5) + rng.integers(0, D)) % D).to(H.DEV)
+        bits = rng.integers(1 << 23, 1 << 24, M) | 0x10101          # a bit at the lower end of every part
+        v = torch.from_numpy(bits * 2.0 ** rng.integers(-40, 10, M).astype(float) * rng.choice([-1, 1], M)).to(H.DEV)
+        x = torch.zeros((M, D), device=H.DEV)
+        x[rows, at] = v.float()
+        emb.emb_rows_product(x, wd, D, got)
+        assert torch.equal(got.double(), v[:, None] * wv[:, at].t()), k
+
+
+@pytest.mark.parametrize("kind,M,N", [("f32", 70, 20_600), ("f32", 49, 20_600), ("bf16", 70, 300), ("bf16", 33, 130)])
+def test_product_of_many_rows_very_far_apart(kind, M, N):
+    # more rows of x than the sizes alone would send to the kernel that takes rows more than 4 MB apart
+    D, stride = 64, 3 << 20
+    rng = np.random.default_rng(M + N)
+    far = torch.full((M, stride), float("nan"), dtype=TORCH[kind], device=H.DEV)
+    x = torch.from_numpy(rng.standard_normal((M, D)).astype(np.float32)).to(TORCH[kind])
+    far[:, :D] = x.to(H.DEV)
+    w = mx.random_rows(rng, N, D, 118, 129)
+    o = torch.empty((M, N), device=H.DEV)
+    emb.emb_rows_product(far[:, :D], H.dev(w), D, o)
+    xv, wv = x.double().numpy(), mx.values(w, D)
+    tol = D * (3 if kind == "f32" else 1) * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T)
+    assert np.all(np.abs(o.cpu().double().numpy() - xv @ wv.T) <= tol)
+
+
+@pytest.mark.parametrize("mode", ["sum", "mean"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("q,D", [("int8", 16), ("int4", 16), ("int4r64", 16), ("int8", 48), ("int4", 80), ("mxfp4", 160), ("int8", 240),
+                                 ("mxfp4", 256), ("int4", 272), ("mxfp4", 320), ("int4r64", 496), ("mxfp4", 544), ("int8", 1008)])
+def test_quantized_cache_of_every_width(q, D, dtype, mode):
+    # every number of lanes to a bag, filled and partly filled, bags from none to several batches of lookups
+    rng = np.random.default_rng(D)
+    R, B = 150, 41
+    t = torch.from_numpy((rng.standard_normal((R, D)) * 2.0 ** rng.integers(-20, 20, (R, 1))).astype(np.float32)).to(TORCH[dtype]).to(H.DEV)
+    lengths = rng.integers(0, 70, B)
+    lengths[[0, 7, B - 1]] = 0, 0, 130
+    off = np.concatenate(([0], np.cumsum(lengths))).astype(np.int64)
+    raw = rng.integers(0, 1 << 63, size=int(off[-1]), dtype=np.int64)
+    rows = torch.empty(raw.size, dtype=torch.int64, device=H.DEV)
+    emb.emb_hash_ids(H.dev(raw), 5, R, rows)
+    hot = np.sort(rng.choice(R, size=90, replace=False)).astype(np.int64)
+    status = torch.zeros(1, dtype=torch.int32, device=H.DEV)
+    hm = torch.zeros(2, dtype=torch.int64, device=H.DEV)
+    cache = torch.empty((hot.size, emb.emb_row_bytes(D, q)), dtype=torch.uint8, device=H.DEV)
+    index = torch.empty(emb.emb_cache_index_bytes(R), dtype=torch.uint8, device=H.DEV)
+    emb.emb_cache_build_quantized(t.data_ptr(), R, D, dtype, q, H.dev(hot), cache, index, status)
+    vals = t.double().cpu().numpy()
+    packed = cache.cpu().numpy()
+    vals[hot] = mx.values(packed, D) if q == "mxfp4" else mx.int_values(packed, D, q)
+    r = rows.cpu().numpy()
+    ref, mag = mx.pool(vals[r], off, mode)
+    n = lengths[:, None]
+    hits = int(np.isin(r, hot).sum())
+    for call, ids in ((emb.emb_bag_forward_cached_quantized, (rows,)), (emb.emb_bag_forward_cached_quantized_hashed, (5, H.dev(raw)))):
+        out = torch.full((1, B, D), 9.0, device=H.DEV)
+        hm.zero_()
+        call(t.data_ptr(), R, D, dtype, q, cache, index, hot.size, *ids, H.dev(off), B, mode, out, hm, status)
+        got = out.cpu().numpy()[0]
+        # a sum's additions and a mean's division, and of INT rows the fused multiply-add, of half a step each
+        assert np.all(np.abs(got - ref) <= (n + 2) * 2.0 ** -24 * mag)
+        assert (got[lengths == 0] == 0).all()
+        assert hm.cpu().tolist() == [hits, r.size - hits]
+    assert status.item() == 0
