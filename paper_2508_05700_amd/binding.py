@@ -582,8 +582,12 @@ def emb_bag_forward_mixed(mt: MixedTables, rows: torch.Tensor, offsets: torch.Te
 
 
 @functools.lru_cache(maxsize=1024)   # (asking the library takes as long as the rest of a call's marshalling)
+def _row_bytes(D: int, dtype: str) -> int:
+    return int(lib().emb_row_bytes(D, DTYPE[dtype]))
+
+
 def emb_row_bytes(D: int, dtype: str) -> int:
-    return int(lib().emb_row_bytes(int(D), DTYPE[dtype]))
+    return _row_bytes(int(D), dtype)   # (by the number: a tensor would be remembered as the object that it is)
 
 
 def emb_quantize_rows(src: torch.Tensor, dtype: str, dst) -> None:
@@ -873,11 +877,15 @@ def emb_bag_backward_rowwise_adagrad(tables: TableSet, rows: torch.Tensor, offse
         _stream()))
 
 
-@functools.lru_cache(maxsize=1024)   # (as emb_row_bytes)
-def emb_cache_index_bytes(num_rows: int) -> int:
+@functools.lru_cache(maxsize=1024)   # (as _row_bytes)
+def _cache_index_bytes(num_rows: int) -> int:
     out = C.c_size_t(0)
-    _check("emb_cache_index_bytes", lib().emb_cache_index_bytes(int(num_rows), C.byref(out)))
+    _check("emb_cache_index_bytes", lib().emb_cache_index_bytes(num_rows, C.byref(out)))
     return int(out.value)
+
+
+def emb_cache_index_bytes(num_rows: int) -> int:
+    return _cache_index_bytes(int(num_rows))
 
 
 def emb_cache_build(table_ptr: int, num_rows: int, D: int, dtype: str, hot_rows: torch.Tensor,
