@@ -1025,6 +1025,23 @@ int dispatch_product(const ProductArgs &a, hipStream_t s)
     }
 }
 
+// W in halves where a launch would have more threads than a grid holds (33 rows of fp32 x by 7e8 rows of W).
+template <int XT, bool OUT_BF16>
+int product_in_launches(ProductArgs a, hipStream_t s)
+{
+    const int rc = dispatch_product<XT, OUT_BF16>(a, s);
+    if (rc != EMB_ERR_UNSUPPORTED || a.N < 4096) return rc;
+    ProductArgs rest = a;
+    a.N = a.N / 2 / 2048 * 2048;                          // (whole tiles)
+    rest.N -= a.N;
+    rest.w += a.N * a.w_pitch;
+    rest.out += a.N * (OUT_BF16 ? 2 : 4);
+    const int half = product_in_launches<XT, OUT_BF16>(a, s);
+    return half != EMB_OK ? half : product_in_launches<XT, OUT_BF16>(rest, s);
+}
+
+constexpr int64_t MOST_ROWS = ((int64_t)1 << 31) - 2048;   // of x and of W: row numbers, tiles of them included, are 32-bit
+
 }  // namespace
 
 extern "C" int emb_rows_product(const void *x_dev, int32_t x_dtype, int64_t x_stride, int64_t M, const void *w_rows_dev, int64_t N,
@@ -1045,16 +1062,16 @@ extern "C" int emb_rows_product(const void *x_dev, int32_t x_dtype, int64_t x_st
     if (M == 0 || N == 0) return EMB_OK;
     if (!x_dev || !w_rows_dev || !out_dev) return EMB_ERR_INVALID_ARG;
     if (!emb_aligned(x_dev, 16) || !emb_aligned(w_rows_dev, 16) || !emb_aligned(out_dev, emb_elem_size(out_dtype))) return EMB_ERR_INVALID_ARG;
-    if (M > (int64_t)0x7FFFFFFF || N > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
+    if (M > MOST_ROWS || N > MOST_ROWS) return EMB_ERR_UNSUPPORTED;
     const ProductArgs a{static_cast<const char *>(x_dev), static_cast<const char *>(w_rows_dev), x_pitch, row, M, N, D,
                         static_cast<char *>(out_dev), out_stride, 0, 0, 1, 0};
     hipStream_t s = emb_stream(stream);
     const bool b = out_dtype == EMB_BF16;
     int e;
     switch (x_dtype) {
-        case EMB_MXFP4: e = b ? dispatch_product<X_MXFP4, true>(a, s) : dispatch_product<X_MXFP4, false>(a, s); break;
-        case EMB_BF16: e = b ? dispatch_product<X_BF16, true>(a, s) : dispatch_product<X_BF16, false>(a, s); break;
-        default: e = b ? dispatch_product<X_F32, true>(a, s) : dispatch_product<X_F32, false>(a, s);
+        case EMB_MXFP4: e = b ? product_in_launches<X_MXFP4, true>(a, s) : product_in_launches<X_MXFP4, false>(a, s); break;
+        case EMB_BF16: e = b ? product_in_launches<X_BF16, true>(a, s) : product_in_launches<X_BF16, false>(a, s); break;
+        default: e = b ? product_in_launches<X_F32, true>(a, s) : product_in_launches<X_F32, false>(a, s);
     }
     if (e != EMB_OK) return e;
     EMB_RETURN_IF_LAUNCH_FAILED();

@@ -143,3 +143,25 @@ def test_quantized_cache_of_every_width(q, D, dtype, mode):
         assert (got[lengths == 0] == 0).all()
         assert hm.cpu().tolist() == [hits, r.size - hits]
     assert status.item() == 0
+
+
+def test_product_of_more_threads_than_a_grid_holds():
+    # 33 rows of fp32 x are three tiles by 128 rows of W: beyond 7.1e8 rows of W more than 2^32 threads
+    M, N, D = 33, 730_000_000, 32
+    rng = np.random.default_rng(9)
+    at = np.unique(np.concatenate((rng.integers(0, N, 300), np.arange(N // 2 - 3000, N // 2 + 3000), [0, N - 1])))
+    w = mx.random_rows(rng, at.size, D, 118, 129)
+    w[:, 0] |= 0x11                                          # (no row of zeros)
+    wd = torch.zeros((N, emb.emb_row_bytes(D, "mxfp4")), dtype=torch.uint8, device=H.DEV)
+    where = torch.from_numpy(at).to(H.DEV)
+    wd[where] = H.dev(w)
+    x = torch.from_numpy(rng.standard_normal((M, D)).astype(np.float32))
+    o = torch.full((M, N), 3.0, dtype=torch.bfloat16, device=H.DEV)
+    emb.emb_rows_product(x.to(H.DEV), wd, D, o)
+    xv, wv = x.double().numpy(), mx.values(w, D)
+    got = o[:, where].cpu().double().numpy()
+    ref, mag = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    tol = 3 * D * 2.0 ** -23 * mag
+    assert np.all(np.abs(got - ref) <= tol + 2.0 ** -8 * (np.abs(ref) + tol))
+    for m in range(M):                                       # every other row of W is zeros
+        assert int(torch.count_nonzero(o[m])) == int(np.count_nonzero(got[m])), m
