@@ -15,6 +15,9 @@ static inline hipStream_t emb_stream(void *s) { return reinterpret_cast<hipStrea
         if (hipGetLastError() != hipSuccess) return EMB_ERR_HIP; \
     } while (0)
 
+// A launch has fewer than 2^32 threads.  So many of `items` with `threads` each are given to one where there may be more.
+static inline int64_t emb_launch_items(int64_t threads) { return ((int64_t)1 << 31) / threads; }
+
 static inline bool emb_aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // Checks shared by the multi-table entry points.  Returns EMB_OK or an error.

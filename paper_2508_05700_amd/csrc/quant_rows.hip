@@ -395,29 +395,25 @@ void dispatch_quantize(const RowsArgs &a)
 }
 
 template <bool BF16>
-int launch_mx_quantize(const RowsArgs &a)
+void launch_mx_quantize(const RowsArgs &a)
 {
     const uint32_t cpr = (uint32_t)a.D * (BF16 ? 2 : 4) / 16, magic = (uint32_t)(((uint64_t)1 << 32) / cpr) + 1u;
     const int64_t chunks = a.R * (int64_t)cpr, blocks = (chunks + MX_BLOCK * MX_UNROLL - 1) / (MX_BLOCK * MX_UNROLL);
-    if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
     if (a.pick)
         hipLaunchKernelGGL((mx_quantize_picked_kernel<BF16>), dim3(pick_grid(chunks)), dim3(PICK_BLOCK), 0, a.s, a.src, a.src_pitch,
                            a.R, (uint32_t)a.D, cpr, magic, (uint32_t)a.row_bytes, a.dst, *a.pick);
     else
         hipLaunchKernelGGL((mx_quantize_kernel<BF16>), dim3((unsigned)blocks), dim3(MX_BLOCK), 0, a.s, a.src, a.src_pitch, a.R,
                            (uint32_t)a.D, cpr, magic, (uint32_t)a.row_bytes, a.dst);
-    return EMB_OK;
 }
 
 template <int FMT, bool BF16>
-int launch_dequantize(const char *src, int64_t R, int32_t D, int64_t row_bytes, char *dst, int64_t dst_pitch, hipStream_t s)
+void launch_dequantize(const char *src, int64_t R, int32_t D, int64_t row_bytes, char *dst, int64_t dst_pitch, hipStream_t s)
 {
     const uint32_t cpr = (uint32_t)D * (BF16 ? 2 : 4) / 16, magic = (uint32_t)(((uint64_t)1 << 32) / cpr) + 1u;
     const int64_t blocks = (R * (int64_t)cpr + MX_BLOCK * MX_UNROLL - 1) / (MX_BLOCK * MX_UNROLL);
-    if (blocks > (int64_t)0x7FFFFFFF) return EMB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((dequantize_rows_kernel<FMT, BF16>), dim3((unsigned)blocks), dim3(MX_BLOCK), 0, s, src, R, (uint32_t)D, cpr,
                        magic, (uint32_t)row_bytes, dst, dst_pitch);
-    return EMB_OK;
 }
 
 // Pitch in bytes of full-precision rows, or 0 if it is none the kernels take.
@@ -433,15 +429,20 @@ inline int64_t plain_pitch(int32_t D, int32_t dtype, int64_t stride)
 int emb_quantize_launch(const void *src, int32_t src_dtype, int64_t src_pitch, int64_t R, int32_t D, int32_t dtype, void *dst,
                         const emb_row_pick *pick, hipStream_t s)
 {
-    const RowsArgs a{static_cast<const char *>(src), src_pitch, R, D, emb_row_bytes(D, dtype), static_cast<char *>(dst), pick, s};
+    const int64_t rb = emb_row_bytes(D, dtype);
     const bool bf16 = src_dtype == EMB_BF16;
-    int rc = EMB_OK;
-    switch (emb_quant_format(dtype)) {
-        case EMB_FMT_INT8: bf16 ? dispatch_quantize<8, true>(a) : dispatch_quantize<8, false>(a); break;
-        case EMB_FMT_INT4: bf16 ? dispatch_quantize<4, true>(a) : dispatch_quantize<4, false>(a); break;
-        default: rc = bf16 ? launch_mx_quantize<true>(a) : launch_mx_quantize<false>(a);
+    // threads of a row: 16 elements each, or (MXFP4) MX_UNROLL times 16 bytes; a launch that picks has a bounded grid
+    const int threads = dtype == EMB_MXFP4 ? (D * emb_elem_size(src_dtype) + 63) / 64 : emb_quant_lanes(D);
+    const int64_t most = pick ? R : emb_launch_items(threads);
+    for (int64_t r = 0; r < R; r += most) {
+        const RowsArgs a{static_cast<const char *>(src) + r * src_pitch, src_pitch, R - r < most ? R - r : most, D, rb,
+                         static_cast<char *>(dst) + r * rb, pick, s};
+        switch (emb_quant_format(dtype)) {
+            case EMB_FMT_INT8: bf16 ? dispatch_quantize<8, true>(a) : dispatch_quantize<8, false>(a); break;
+            case EMB_FMT_INT4: bf16 ? dispatch_quantize<4, true>(a) : dispatch_quantize<4, false>(a); break;
+            default: bf16 ? launch_mx_quantize<true>(a) : launch_mx_quantize<false>(a);
+        }
     }
-    if (rc != EMB_OK) return rc;
     EMB_RETURN_IF_LAUNCH_FAILED();
     return EMB_OK;
 }
@@ -472,7 +473,7 @@ extern "C" int emb_dequantize_rows(const void *src_dev, int32_t dtype, int64_t n
                                    int64_t dst_stride, void *stream)
 {
     if (num_rows < 0) return EMB_ERR_INVALID_ARG;
-    int rc = emb_check_quant_rows(D, dtype);
+    const int rc = emb_check_quant_rows(D, dtype);
     if (rc != EMB_OK) return rc;
     const int64_t pitch = plain_pitch(D, dst_dtype, dst_stride);
     if (pitch == 0) return EMB_ERR_INVALID_ARG;
@@ -483,16 +484,19 @@ extern "C" int emb_dequantize_rows(const void *src_dev, int32_t dtype, int64_t n
     char *dst = static_cast<char *>(dst_dev);
     const int64_t rb = emb_row_bytes(D, dtype);
     hipStream_t s = emb_stream(stream);
-#define EMB_DQ(FMT)                                                                                 \
-    rc = dst_dtype == EMB_BF16 ? launch_dequantize<FMT, true>(src, num_rows, D, rb, dst, pitch, s) \
-                               : launch_dequantize<FMT, false>(src, num_rows, D, rb, dst, pitch, s)
-    switch (emb_quant_format(dtype)) {
-        case EMB_FMT_INT8: EMB_DQ(EMB_FMT_INT8); break;
-        case EMB_FMT_INT4: EMB_DQ(EMB_FMT_INT4); break;
-        default: EMB_DQ(EMB_FMT_MXFP4);
+    const int64_t most = emb_launch_items((D * emb_elem_size(dst_dtype) + 63) / 64);
+#define EMB_DQ(FMT)                                                                                                  \
+    dst_dtype == EMB_BF16 ? launch_dequantize<FMT, true>(src + r * rb, n, D, rb, dst + r * pitch, pitch, s)          \
+                          : launch_dequantize<FMT, false>(src + r * rb, n, D, rb, dst + r * pitch, pitch, s)
+    for (int64_t r = 0; r < num_rows; r += most) {
+        const int64_t n = num_rows - r < most ? num_rows - r : most;
+        switch (emb_quant_format(dtype)) {
+            case EMB_FMT_INT8: EMB_DQ(EMB_FMT_INT8); break;
+            case EMB_FMT_INT4: EMB_DQ(EMB_FMT_INT4); break;
+            default: EMB_DQ(EMB_FMT_MXFP4);
+        }
     }
 #undef EMB_DQ
-    if (rc != EMB_OK) return rc;
     EMB_RETURN_IF_LAUNCH_FAILED();
     return EMB_OK;
 }

@@ -165,3 +165,23 @@ def test_product_of_more_threads_than_a_grid_holds():
     assert np.all(np.abs(got - ref) <= tol + 2.0 ** -8 * (np.abs(ref) + tol))
     for m in range(M):                                       # every other row of W is zeros
         assert int(torch.count_nonzero(o[m])) == int(np.count_nonzero(got[m])), m
+
+
+def test_int_rows_of_more_threads_than_a_grid_holds():
+    # 64 threads a row of 528 elements: beyond 6.7e7 rows more than 2^32
+    R, D, k, q = 68_000_000, 528, 300, "int4"
+    rng = np.random.default_rng(10)
+    at = np.unique(np.concatenate((rng.integers(0, R, k), np.arange((1 << 25) - k, (1 << 25) + k), np.arange((1 << 26) - k, (1 << 26) + k),
+                                   np.arange(R - k, R))))
+    where = torch.from_numpy(at).to(H.DEV)
+    t = torch.from_numpy(rng.standard_normal((at.size, D)).astype(np.float32)).to(torch.bfloat16).to(H.DEV)
+    src = torch.ones((R, D), dtype=torch.bfloat16, device=H.DEV)
+    src[where] = t
+    rows = torch.zeros((R, emb.emb_row_bytes(D, q)), dtype=torch.uint8, device=H.DEV)
+    emb.emb_quantize_rows_from(src, q, rows)
+    want = torch.empty((at.size, rows.shape[1]), dtype=torch.uint8, device=H.DEV)
+    emb.emb_quantize_rows_from(t, q, want)
+    assert torch.equal(rows[where], want)
+    # (every other row is constant: scale and bias 1, codes 0)
+    header = rows[:, :8].contiguous().view(torch.float32)
+    assert int((header == 1).all(1).sum()) == R - at.size
