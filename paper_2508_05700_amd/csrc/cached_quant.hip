@@ -251,16 +251,19 @@ template <int FMT, bool BF16>
 void launch_cached_either(const QuantCachedArgs &a)
 {
 #define EMB_CE(L, E)                                                                                                     \
-    hipLaunchKernelGGL((bag_forward_cached_either_kernel<L, FMT, E, BF16>),                                              \
-                       dim3((unsigned)((a.B + Q_BLOCK / L - 1) / (Q_BLOCK / L))), dim3(Q_BLOCK), 0, a.s, a.src, a.B,      \
-                       a.nnz, a.ids, a.offsets, a.D, a.mode, a.out, a.hit_miss, a.status)
-    if (a.D <= 16) EMB_CE(2, 8);
-    else if (a.D <= 32) EMB_CE(4, 8);
-    else if (a.D <= 64) EMB_CE(8, 8);
-    else if (a.D <= 128) EMB_CE(16, 8);
-    else if (a.D <= 256) EMB_CE(32, 8);
-    else if (a.D <= 512) EMB_CE(64, 8);
-    else EMB_CE(64, 16);
+    for (int64_t b = 0; b < a.B; b += emb_launch_items(L)) {                                                             \
+        const int64_t n = a.B - b < emb_launch_items(L) ? a.B - b : emb_launch_items(L);                                 \
+        hipLaunchKernelGGL((bag_forward_cached_either_kernel<L, FMT, E, BF16>),                                          \
+                           dim3((unsigned)((n + Q_BLOCK / L - 1) / (Q_BLOCK / L))), dim3(Q_BLOCK), 0, a.s, a.src, n,      \
+                           a.nnz, a.ids, a.offsets + b, a.D, a.mode, a.out + b * a.D, a.hit_miss, a.status);             \
+    }
+    if (a.D <= 16) EMB_CE(2, 8)
+    else if (a.D <= 32) EMB_CE(4, 8)
+    else if (a.D <= 64) EMB_CE(8, 8)
+    else if (a.D <= 128) EMB_CE(16, 8)
+    else if (a.D <= 256) EMB_CE(32, 8)
+    else if (a.D <= 512) EMB_CE(64, 8)
+    else EMB_CE(64, 16)
 #undef EMB_CE
 }
 

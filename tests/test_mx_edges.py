@@ -185,3 +185,36 @@ def test_int_rows_of_more_threads_than_a_grid_holds():
     # (every other row is constant: scale and bias 1, codes 0)
     header = rows[:, :8].contiguous().view(torch.float32)
     assert int((header == 1).all(1).sum()) == R - at.size
+
+
+def test_quantized_cache_of_more_threads_than_a_grid_holds():
+    # 64 threads a bag of 272 elements: beyond 6.7e7 bags more than 2^32.  A few bags have lookups, at both ends and where one
+    # launch ends and the next begins.
+    B, D, R, q = 68_000_000, 272, 50, "int8"
+    rng = np.random.default_rng(11)
+    t = torch.from_numpy(rng.standard_normal((R, D)).astype(np.float32)).to(H.DEV)
+    hot = np.arange(0, R, 2, dtype=np.int64)
+    cache = torch.empty((hot.size, emb.emb_row_bytes(D, q)), dtype=torch.uint8, device=H.DEV)
+    index = torch.empty(emb.emb_cache_index_bytes(R), dtype=torch.uint8, device=H.DEV)
+    status, hm = torch.zeros(1, dtype=torch.int32, device=H.DEV), torch.zeros(2, dtype=torch.int64, device=H.DEV)
+    emb.emb_cache_build_quantized(t.data_ptr(), R, D, "f32", q, H.dev(hot), cache, index, status)
+    bags = np.unique(np.concatenate([np.arange(c, c + 40) for c in (0, (1 << 25) - 20, (1 << 26) - 20, B - 40)]))
+    where = torch.from_numpy(bags).to(H.DEV)
+    lengths = torch.zeros(B + 1, dtype=torch.int64, device=H.DEV)
+    lengths[where + 1] = torch.arange(bags.size, device=H.DEV) % 5
+    off = torch.cumsum(lengths, 0)
+    rows = rng.integers(0, R, int(off[-1])).astype(np.int64)
+    out = torch.full((1, B, D), 9.0, device=H.DEV)
+    emb.emb_bag_forward_cached_quantized(t.data_ptr(), R, D, "f32", q, cache, index, hot.size, H.dev(rows), off, B, "sum", out, hm, status)
+    vals = t.double().cpu().numpy()
+    vals[hot] = mx.int_values(cache.cpu().numpy(), D, q)
+    n = np.arange(bags.size) % 5
+    ref, mag = mx.pool(vals[rows], np.concatenate(([0], np.cumsum(n))), "sum")
+    got = out[0, where].cpu().numpy()
+    assert np.all(np.abs(got - ref) <= (n[:, None] + 2) * 2.0 ** -24 * mag)
+    hits = int(np.isin(rows, hot).sum())
+    assert hm.cpu().tolist() == [hits, rows.size - hits] and status.item() == 0
+    used = 0
+    for b0 in range(0, B, 1 << 23):                          # every other bag is empty
+        used += int(torch.count_nonzero(out[0, b0:b0 + (1 << 23)].any(1)))
+    assert used == np.count_nonzero(got.any(1))
