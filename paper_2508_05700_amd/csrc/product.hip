@@ -376,7 +376,10 @@ __device__ __forceinline__ bool tile_of(const ProductArgs &a, uint32_t &tm, uint
 
 // Short rows make much more output than input, and reads of W that trickle in between the writes slow both.  So a die's first
 // workgroups, one for each of its CUs, read its part of W at once (a word of every line, to no use), which brings it to the memory-side cache: with W
-// in HBM 512 x 200000 x 128 from MXFP4 67 us, so 53; with W in the cache already 42.5 and 44.
+// in HBM 512 x 200000 x 128 from MXFP4 67 us, so 47; with W in the cache already 42.5 and 44.  A larger W is out of that cache again
+// before it is used, and is read twice: 128 x 600000 x 128 (48 MB) 55 us, so 47; 128 x 1200000 x 64 (58 MB) 100 and 95; 512 x 800000 x 128
+// (64 MB) 251 and 260; 128 x 1000000 x 128 (80 MB) 87 and 94; 128 x 4000000 x 128 (320 MB) 347 and 409.  So up to MOST_EARLY bytes of it.
+constexpr int64_t MOST_EARLY = 48 << 20;
 template <int BN, int THREADS>
 __device__ __forceinline__ uint32_t early_rows(const ProductArgs &a)
 {
@@ -604,7 +607,8 @@ inline int64_t share_tiles(ProductArgs &a, int64_t bm, int64_t bn)
             a.die_rows = rows;
         }
     }
-    a.early = a.D <= 128 && best > 128;   // (a die holds up to 128 workgroups at once: fewer read W at once anyway)
+    // (a die holds up to 128 workgroups at once: fewer read W at once anyway)
+    a.early = a.D <= 128 && best > 128 && a.N * a.w_pitch <= MOST_EARLY;
     return best * EMB_XCDS;
 }
 

@@ -218,3 +218,30 @@ def test_quantized_cache_of_more_threads_than_a_grid_holds():
     for b0 in range(0, B, 1 << 23):                          # every other bag is empty
         used += int(torch.count_nonzero(out[0, b0:b0 + (1 << 23)].any(1)))
     assert used == np.count_nonzero(got.any(1))
+
+
+@pytest.mark.parametrize("kind", ["mxfp4", "bf16", "f32"])
+@pytest.mark.parametrize("M,N,D", [(65, 1_000_000, 64), (65, 1_100_000, 64), (70, 600_000, 96), (129, 700_001, 128)])
+def test_product_of_short_rows_on_both_sides_of_the_early_read(M, N, D, kind):
+    # W of 38 to 56 MB (its rows are read ahead up to 48 MiB): sums of 4 integers, exact
+    rng = np.random.default_rng(N + D)
+    codes = torch.randint(0, 16, (N, D // 2, 2), dtype=torch.uint8, device=H.DEV, generator=torch.Generator(H.DEV).manual_seed(N))
+    w = torch.zeros((N, emb.emb_row_bytes(D, "mxfp4")), dtype=torch.uint8, device=H.DEV)
+    w[:, :D // 2] = codes[:, :, 0] | codes[:, :, 1] << 4
+    w[:, D // 2:D // 2 + D // 32] = 128
+    values = torch.tensor([0, 1, 2, 3, 4, 6, 8, 12], dtype=torch.float32, device=H.DEV)     # at this scale
+    v = (values[(codes & 7).long()] * (1 - 2 * (codes >> 3).float())).reshape(N, D)
+    x = torch.zeros((M, D), device=H.DEV)
+    at = torch.from_numpy(np.argsort(rng.random((M, D)), 1)[:, :4].copy()).to(H.DEV)
+    x.scatter_(1, at, torch.from_numpy(rng.choice([-2.0, -1.0, 1.0, 2.0], (M, 4)).astype(np.float32)).to(H.DEV))
+    o = torch.full((M, N), 0.5, device=H.DEV)
+    if kind == "mxfp4":
+        small = torch.empty((M, w.shape[1]), dtype=torch.uint8, device=H.DEV)
+        emb.emb_quantize_rows_from(x, "mxfp4", small)
+        emb.emb_rows_product(small, w, D, o)
+    else:
+        emb.emb_rows_product(x.to(TORCH[kind]), w, D, o)
+    for m in range(0, M, 8):
+        ref = sum(x[m, k] * v[:, k] for k in at[m].tolist())
+        assert torch.equal(o[m], ref), m
+    assert not (o == 0.5).any()
