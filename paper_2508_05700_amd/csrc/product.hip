@@ -954,19 +954,22 @@ int launch_skinny(ProductArgs a, hipStream_t s)
 //   are very few (1 x 4096 x 4096 bf16 5.1, without 9.3; 8 x 512 x 16384 fp32 25, with 8 ways 39).  Beyond about 1024 tiles the other
 //   kernels fill it (16 x 50000 x 512 bf16 5.3, split 12.9); the split parts of fp32, for which every wavefront makes three parts of its
 //   x, lose from 512 on (1024 x 512 x 1024 8.9, split 18.8); few rows of MXFP4 that are very long, which have no other kernel that shares
-//   a tile, gain up to 2048 (32 x 16384 x 4096 16.5, without 31).
+//   a tile, gain up to 1536 (8 x 33792 x 4096 20.2, without 29.5; 16 x 49152 x 4096 28.2 and 34.9; 8 x 33792 x 2048 12.9 and 15.3, but 32 x 24576
+//   x 2048 14.1 and 12.4), and lose at 2048 (32 x 32768 x 4096 31.6 and 25.2, 1 x 65536 x 2048 20.1 and 16.7).
 //   Few rows of x: W streams through registers; MXFP4 and short rows straight from global memory (16 x 100003 x 64 fp32 6.4,
 //   through LDS 8.5; from 256 elements on LDS is ahead: 16 x 100003 x 512 bf16 8.9, straight 11.6, fp32 11.9 and 19.4), others with x in
 //   LDS (16 x 128000 x 2048 bf16 37, straight 50).  33 to 64 rows of MXFP4 are tiles where they are long and W has not rows enough for
 //   straight wavefronts (64 x 16384 x 4096 16.5, straight 31; 64 x 128000 x 2048 44, tiles 50).
 //   A row of x costs an fp32 product three MFMA, and the tiles for it are the less efficient: three passes over W are still quicker
 //   than one over half-empty tiles (48 x 128000 x 2048: 114 and 188), and any number of them where tiles do not fill the
-//   chip once (256 x 4096 x 1024 12.2, tiles 38.6; 512 x 2048 x 4096 46 and 142; the shorter the rows, the sooner tiles are ahead: 256 x 16384 x 256
-//   16.4 and 13.9, 512 x 4096 x 256 9.5 and 12.9).  bf16 takes half tiles there (512 x 4096 x 4096 29, whole 37.6).
+//   chip once (256 x 4096 x 1024 12.2, tiles 38.6; 512 x 2048 x 4096 46 and 142; the shorter the rows, the sooner tiles are ahead.  512
+//   elements: 256 x 24576 28.9 and 33.4, 256 x 32768, 512 tiles, 36.9 and 34.6; 128 elements: 256 x 8192 8.8 and 9.5, 256 x 10240, 160 tiles, 10.2 and
+//   9.9; between them a line at 160 is early for some, at 256 late for others: 256 x 10240 x 384 13.0 and 18.2, 256 x 15000 x 256 16.0 and 14.3).  bf16 takes half tiles there (512 x 4096 x 4096 29, whole 37.6).
 //   Rows of x so far apart that 128 of them pass 32-bit offsets: LDS as well, any number of rows.
 //   Up to 32 rows of x past whole tiles: a call of their own, where their tiles would begin another round of workgroups on the
 //   chip (at_once of them) and rows are long enough for that to take longer than the call (4099 rows of x, 4096 of W: 1024 elements
-//   bf16 45.2, so 42.7, fp32 180, so 163; 4096: MXFP4 63.8, so 44.1, bf16 167, so 142; with 512 elements bf16 nothing is won).
+//   bf16 45.2, so 42.7, fp32 180, so 163; 4096: MXFP4 63.8, so 44.1, bf16 167, so 142; with 512 elements bf16 nothing is won).  MXFP4 up to 65536
+//   rows of W: 4099 x 32768 x 1024 148, so 145; 4099 x 61440 x 1024 254 and 253; 4099 x 131072 x 1024 547 and 561, 2050 x 131072 x 2048 432 and 456.
 inline int64_t rows_of_full_rounds(const ProductArgs &a, int64_t tile, int64_t at_once)
 {
     const int64_t whole = a.M / tile * tile, rest = a.M - whole;
@@ -996,7 +999,7 @@ template <int XT, bool OUT_BF16>
 int dispatch_product(const ProductArgs &a, hipStream_t s)
 {
     const int64_t tiles = (a.M + 15) / 16 * ((a.N + 31) / 32);
-    const int64_t most_split = XT == X_F32 ? 512 : (XT == X_MXFP4 && a.M <= 32 && a.D >= 2048 ? 2048 : 1024);
+    const int64_t most_split = XT == X_F32 ? 512 : (XT == X_MXFP4 && a.M <= 32 && a.D >= 2048 ? 1536 : 1024);
     if (a.D > 512 && tiles <= most_split) return tiles < 256 ? launch_direct<XT, 1, 1, 16, OUT_BF16>(a, s) : launch_direct<XT, 1, 2, 8, OUT_BF16>(a, s);
     if constexpr (XT == X_MXFP4) {
         if (a.M <= 16) return launch_direct<XT, 1, 2, 1, OUT_BF16>(a, s);
