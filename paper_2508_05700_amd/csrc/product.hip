@@ -8,7 +8,7 @@
 // exact, sums are fp32.  With x in bf16, W's elements become bf16, exactly, and the product is
 // bf16's.  With x in fp32, x = h + m + l with three bf16 parts of 8 bits each, exact unless a
 // part falls below bf16's range: three bf16 products with the same W, summed in fp32 from the smallest part on.
-// (Infinite elements of W are for redo_infinite_rows.)
+// (Infinite elements of W are for mend_infinite_rows.)
 //
 // A wavefront holds a tile of 16*NT rows of W and 16*MT rows of x.  W is the unit's
 // row operand, so that a lane ends with four neighbouring n of one m: one 16-byte store.
@@ -134,50 +134,60 @@ __device__ __forceinline__ void split_bf16(const uint4 &a, const uint4 &b, mx_b8
 
 // Rows of W with infinite elements (under a scale byte of 253 or 254: 4 and 6 by 2^126, 2 to 6 by 2^127; the quantisers here
 // write none) and an fp32 x.  A part of x that is zero makes NaN of an infinity, where fp32 has the infinity that the other parts
-// make of it (theirs have the same sign, so nothing but NaN is ever wrong).  A wavefront with a NaN among its sums therefore
-// looks at such results in its tile again, and makes those of rows with such bytes an element of x at a time.  (Seen at the
-// end of a tile, for nothing: a maximum of the scale bytes kept along the way took 2 to 3 % of 4096 x 4096 x 1024.)
-template <int ROWS, int COLS, bool OUT_BF16>
-__device__ __forceinline__ void redo_infinite_rows(const ProductArgs &a, int64_t m0, int64_t n0)
+// make of it (theirs have the same sign, so nothing but NaN is ever wrong).  So a lane with a NaN among its sums makes
+// that of a row with such bytes once more, an element of x at a time.  (Looking at the sums at the end of a tile takes up to 1 %; a
+// maximum of the scale bytes kept along the way took 2 to 3 % of 4096 x 4096 x 1024.  16 x 100003 x 2048: 46 us, with a NaN in x 67, with a
+// row of infinities in W 89; one of NaN 45.)
+template <bool OUT_BF16>
+__device__ __forceinline__ void redo_infinite_row(const ProductArgs &a, int64_t m, int64_t n)
 {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what the wavefront has stored is in its place
-    for (int at = threadIdx.x & 63; at < ROWS * COLS; at += 64) {
-        const int64_t m = m0 + at / COLS, n = n0 + at % COLS;
-        if (m >= a.M || n >= a.N) continue;
-        float *const o32 = reinterpret_cast<float *>(a.out) + m * a.out_stride + n;
-        __bf16 *const o16 = reinterpret_cast<__bf16 *>(a.out) + m * a.out_stride + n;
-        const float was = OUT_BF16 ? (float)*o16 : *o32;
-        if (was == was) continue;
-        const char *const w = a.w + n * a.w_pitch, *const scales = w + a.D / 2, *const x = a.x + m * a.x_pitch;
-        bool infinite = false;
-        for (int b = 0; b < a.D / 32; ++b) infinite |= *(const EMB_GLOBAL uint8_t *)(scales + b) - 253u < 2u;
-        if (!infinite) continue;
-        float sum = 0.f;
-        for (int c = 0; c < a.D / 4; ++c) {            // 4 elements
-            const uint32_t codes = *(const EMB_GLOBAL uint16_t *)(w + 2 * c), byte = *(const EMB_GLOBAL uint8_t *)(scales + c / 8);
-            const float scale = __uint_as_float(byte << 23);
-            const emb_f2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
-            const uint4 v = load_chunk(x + 16 * c);
-            sum = __builtin_fmaf(__uint_as_float(v.x), lo.x, sum);
-            sum = __builtin_fmaf(__uint_as_float(v.y), lo.y, sum);
-            sum = __builtin_fmaf(__uint_as_float(v.z), hi.x, sum);
-            sum = __builtin_fmaf(__uint_as_float(v.w), hi.y, sum);
-        }
-        if (OUT_BF16) *o16 = (__bf16)sum;
-        else *o32 = sum;
+    const char *const w = a.w + n * a.w_pitch, *const scales = w + a.D / 2, *const x = a.x + m * a.x_pitch;
+    bool infinite = false;                             // (or not even so: a byte of the padding)
+    for (int b = 0; b < a.D / 32; b += 16) {
+        const uint4 v = load_chunk(scales + b);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) infinite |= ((word_of(v, k / 4) >> (8 * (k % 4))) & 255u) - 253u < 2u;
     }
+    if (!infinite) return;
+    float sum = 0.f;
+    for (int c = 0; c < a.D / 4; ++c) {                // 4 elements
+        const uint32_t codes = *(const EMB_GLOBAL uint16_t *)(w + 2 * c), byte = *(const EMB_GLOBAL uint8_t *)(scales + c / 8);
+        const float scale = __uint_as_float(byte << 23);
+        const emb_f2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+        const uint4 v = load_chunk(x + 16 * c);
+        sum = __builtin_fmaf(__uint_as_float(v.x), lo.x, sum);
+        sum = __builtin_fmaf(__uint_as_float(v.y), lo.y, sum);
+        sum = __builtin_fmaf(__uint_as_float(v.z), hi.x, sum);
+        sum = __builtin_fmaf(__uint_as_float(v.w), hi.y, sum);
+    }
+    if (OUT_BF16) reinterpret_cast<__bf16 *>(a.out)[m * a.out_stride + n] = (__bf16)sum;
+    else reinterpret_cast<float *>(a.out)[m * a.out_stride + n] = sum;
 }
-// acc: the wavefront's sums, stored; every lane calls this.
+// acc: the lane's sums of rows m0 + 16 * i + r of x, tiles from place n0 on, which it has stored.
 template <int XT, bool OUT_BF16, int MT, int NT>
-__device__ __forceinline__ void mend_infinite_rows(const ProductArgs &a, int64_t m0, int64_t n0, const mx_f4 (&acc)[MT][NT])
+__device__ __forceinline__ void mend_infinite_rows(const ProductArgs &a, int64_t m0, int64_t n0, int r, int g, const mx_f4 (&acc)[MT][NT])
 {
     if constexpr (XT == X_F32) {
-        bool nan = false;
+        static_assert(MT * NT <= 16, "a bit a sum");
+        constexpr int V = NT % TILES<OUT_BF16> == 0 ? TILES<OUT_BF16> : 1;   // as in store_tiles
+        bool any = false;
 #pragma unroll
-        for (int i = 0; i < MT * NT; ++i)
+        for (int i = 0; i < MT * NT; ++i) {            // (two sums a comparison)
+            const mx_f4 v = acc[i / NT][i % NT];
+            any |= __builtin_isunordered(v[0], v[1]) | __builtin_isunordered(v[2], v[3]);
+        }
+        if (!any) return;
+        uint64_t nan = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) nan |= acc[i / NT][i % NT][k] != acc[i / NT][i % NT][k];
-        if (__any(nan)) redo_infinite_rows<16 * MT, 16 * NT, OUT_BF16>(a, m0, n0);
+        for (int i = 0; i < 4 * MT * NT; ++i) {
+            const float v = acc[i / 4 / NT][i / 4 % NT][i % 4];
+            if (v != v) nan |= UINT64_C(1) << i;
+        }
+        for (; nan; nan &= nan - 1) {
+            const int i = __ffsll((unsigned long long)nan) - 1, t = i / 4 % NT;
+            const int64_t m = m0 + 16 * (i / 4 / NT) + r, n = n0 + 16 * V * (t / V) + 4 * V * g + 4 * (t % V) + i % 4;
+            if (m < a.M && n < a.N) redo_infinite_row<OUT_BF16>(a, m, n);
+        }
     }
 }
 
@@ -316,7 +326,7 @@ __global__ __launch_bounds__(KS > 1 ? 64 * KS : 256) void product_direct_kernel(
                 if (n0 + 4 * g + k < a.N) o[k] = (__bf16)acc[i][0][k];
         }
     }
-    mend_infinite_rows<XT, OUT_BF16>(a, m0, n0, acc);
+    mend_infinite_rows<XT, OUT_BF16>(a, m0, n0, r, g, acc);
 }
 
 // A grid holds fewer than 2^32 threads.
@@ -626,7 +636,7 @@ int launch_tiled(ProductArgs a, hipStream_t s)
 // takes the stage's elements from g * STAGE / 4 on, in steps of 8: chunk c of a row of x stands at place c ^ wide_key_x(row).
 // Tiles are 128 x 128.  bf16: by wavefronts of 128 x 32, so that W's codes are widened once; two workgroups fill a CU's LDS
 // exactly.  fp32: by wavefronts of 32 x 128, so that every element of x is split into its three parts once.
-// 8192 x 8192 x 4096 bf16 1.0 PFLOP/s; 4096 x 4096 x 1024 bf16 38 us, fp32 144: what keeps them from the matrix unit's rate is the vector
+// 8192 x 8192 x 4096 bf16 1.0 PFLOP/s; 4096 x 4096 x 1024 bf16 38 us, fp32 122 to 144 by card: what keeps them from the matrix unit's rate is the vector
 // work between its instructions (widening W; for fp32 six operations for an element's parts).
 // Keys for rows of 256 bytes, chunks 4 apart in neighbouring lane groups, and of 64 bytes, chunks 1 apart.
 __device__ __forceinline__ int wide_key_x(int row) { return (row & 3) | ((row >> 1) & 4) | (((row << 1) ^ row) & 8); }
@@ -797,7 +807,7 @@ __global__ __launch_bounds__(256, 2) void product_widened_kernel(ProductArgs a)
     for (int i = 0; i < MT; ++i) {
         store_tiles<NT, OUT_BF16>(a, m0 + wm * MT * 16 + 16 * i + r, n0 + wn * NT * 16, g, acc[i]);
     }
-    mend_infinite_rows<XT, OUT_BF16>(a, m0 + wm * MT * 16, n0 + wn * NT * 16, acc);
+    mend_infinite_rows<XT, OUT_BF16>(a, m0 + wm * MT * 16, n0 + wn * NT * 16, r, g, acc);
 }
 
 template <int XT, bool HALF, bool OUT_BF16>
@@ -928,7 +938,7 @@ __global__ __launch_bounds__(256) void product_skinny_kernel(ProductArgs a, int 
     for (int i = 0; i < MT; ++i) {
         store_tiles<NT, OUT_BF16>(a, m0 + 16 * i + r, n0, g, acc[i]);
     }
-    mend_infinite_rows<XT, OUT_BF16>(a, m0, n0, acc);
+    mend_infinite_rows<XT, OUT_BF16>(a, m0, n0, r, g, acc);
 }
 
 template <int XT, int MT, bool OUT_BF16>
