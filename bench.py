@@ -40,19 +40,19 @@ def log(*a):
 # bytes or less are counted at their true size, so for kernels that issue those (4-byte accumulators,
 # 48-byte quantised rows) the scaled figure is an upper bound.
 PMC_TRAFFIC = {
-    "sources": "445dbbf400e8fb86",
+    "sources": "b9ff888e7b44be50",
     "fetch_scale": 2.0,
     "write_scale": 1.0,
     "kib_per_launch": {     # workload -> kernel -> (FETCH_SIZE, WRITE_SIZE)
-        "3": {"bag_forward_train_kernel": (173324.8, 69748.9), "update_kernel": (240613.9, 324004.0)},
-        "3b": {"bag_forward_train_kernel": (90494.7, 73991.4), "update_kernel": (170033.2, 220969.5)},
-        "2": {"bag_forward_kernel<HASHED>": (172110.4, 33875.4), "bag_forward_kernel": (172180.1, 32768.0)},
-        "2u": {"bag_forward_kernel<HASHED>": (338205.7, 33799.4), "bag_forward_kernel": (338157.7, 32768.0)},
-        "2un": {"bag_forward_kernel": (339629.8, 32768.0)},
-        "2q4": {"bag_forward_quant_kernel": (112585.3, 33832.8)},
-        "2uq4": {"bag_forward_quant_kernel": (224866.8, 33904.1)},
-        "2uq4r": {"bag_forward_quant_kernel": (182427.6, 33863.3)},
-        "4": {"bag_forward_kernel<HASHED>": (52451.3, 8704.3)},
+        "3": {"bag_forward_train_kernel": (173343.4, 69736.7), "update_kernel": (240603.3, 324004.3)},
+        "3b": {"bag_forward_train_kernel": (90531.7, 74070.9), "update_kernel": (170106.7, 220986.6)},
+        "2": {"bag_forward_kernel<HASHED>": (172122.6, 33875.4), "bag_forward_kernel": (172175.7, 32768.0)},
+        "2u": {"bag_forward_kernel<HASHED>": (338202.0, 33799.6), "bag_forward_kernel": (338157.8, 32768.0)},
+        "2un": {"bag_forward_kernel": (339644.6, 32768.0)},
+        "2q4": {"bag_forward_quant_kernel": (112557.9, 33834.9)},
+        "2uq4": {"bag_forward_quant_kernel": (224901.3, 33902.3)},
+        "2uq4r": {"bag_forward_quant_kernel": (182387.6, 33864.5)},
+        "4": {"bag_forward_kernel<HASHED>": (52459.8, 8704.3)},
     },
 }
 
